@@ -47,9 +47,12 @@ extern "C" {
 #endif
 
 typedef uint16_t specee_half;
+typedef uint8_t specee_f8; /* e4m3: sign, 4 bits of exponent (bias 7), 3 of mantissa, no infinity, largest 448 */
 
 #define SPECEE_KMAX 16    /* speculative tokens per token / node */
 #define SPECEE_HMAX 2048  /* predictor hidden width */
+#define SPECEE_IDS_MAX 64 /* tokens per row of specee_logprobs */
+#define SPECEE_TOP_MAX 32 /* alternatives per row of specee_logprobs */
 
 typedef enum specee_status {
     SPECEE_OK = 0,
@@ -89,7 +92,9 @@ typedef enum specee_op {
     SPECEE_OP_VERIFY = 4,
     SPECEE_OP_LAYER_LOOP = 5,
     SPECEE_OP_VERIFY_Q4 = 6,
-    SPECEE_OP_PREDICT_TREE_Q4 = 7
+    SPECEE_OP_PREDICT_TREE_Q4 = 7,
+    SPECEE_OP_LOGPROBS = 8,
+    SPECEE_OP_MATMUL_F8 = 9
 } specee_op;
 
 /*
@@ -338,6 +343,66 @@ int specee_layer_loop_q4(const specee_dims *dims, int L, int B, const specee_hal
                          const int32_t *active, float *logits, float *probs, float *scores, int32_t *exit_flags,
                          int32_t *ver_token, int32_t *hit, int32_t *exit_layer, int32_t *token, int32_t *status,
                          long long spin_limit, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * What stands between two blocks of the model whose hidden states the calls above read: the norm behind a
+ * block, its gate and residual scale, the residual sum, and the norm before what comes next.  For each row,
+ * with r(v) = 1 / sqrt(mean(v^2) + dims->eps):
+ *     t = branch * r(branch) * gamma_post        (gamma_post NULL: t = branch)
+ *     s = hidden_scale * hidden + branch_scale * gate * t
+ *     x = s * r(s) * gamma
+ *   hidden [N][d]; branch [N][d] or NULL (s = hidden_scale * hidden; gamma_post and gate are then NULL too);
+ *   gate [gate_rows][d] or NULL: gate_rows 1 (one for all rows) or N (one per row), ignored without a gate;
+ *   gamma [d], NULL only if no x is asked for.
+ *   hidden_out [N][d] or NULL: s rounded to fp16; may be `hidden` itself, or `branch`.
+ *   x [N][d] or NULL: x rounded to fp16 (from s before its rounding); may be `branch` or `hidden` itself, not
+ *   hidden_out.
+ *   x8 [N][d], x8_scales [N][ceil(d/128)], both or neither NULL: x in 8 bits.  The 128 elements of a block
+ *   (fewer in the last) share scale = max|x| / 448 (1 if they are all 0), and x8 = e4m3(x / scale), to nearest,
+ *   ties to even.  A NaN stays one; an infinity makes its block NaN.
+ * Only dims->d and dims->eps are read.  Needs no workspace.
+ */
+int specee_block_norm(const specee_dims *dims, int N, const specee_half *hidden, const specee_half *branch,
+                      const specee_half *gamma_post, const specee_half *gate, int gate_rows, float hidden_scale,
+                      float branch_scale, const specee_half *gamma, specee_half *hidden_out, specee_half *x,
+                      specee_f8 *x8, float *x8_scales, void *stream);
+
+/*
+ * What is answered with rows of logits (of lm_head_gemv, lm_head_gemv_q4, specee_matmul_f8): the log
+ * probabilities of given tokens, the entropy, the best alternatives.  For each row, with m its largest logit
+ * and S = sum exp(x - m):
+ *     log p(v) = (x_v - m) - log S,      entropy = log S - sum exp(x - m)(x - m) / S.
+ *   logits, logits_f16: one of them, the other NULL; row n starts `stride` elements (>= V) behind row n - 1.
+ *   The pointer needs its type's alignment only.
+ *   ids [N][T] (T up to SPECEE_IDS_MAX; 0: none, ids and logprobs NULL).
+ *   logprobs [N][T]; max_logit (m), log_sum (log S), entropy [N], each or NULL; top_ids, top_logprobs
+ *   [N][n_top] (n_top up to SPECEE_TOP_MAX; 0: none, both NULL): the largest logits, the lower id first among
+ *   equals.  A logit of -inf (a token that is not allowed) has no probability, adds nothing and is no
+ *   alternative: places that remain hold -1 and -inf.
+ * Rows and ids that mean nothing: a row of -inf alone has m, log S and every log probability -inf and entropy 0;
+ * a NaN or +inf in a row makes all its outputs NaN, its top_ids -1; the log probability of an id outside
+ * [0, V) is NaN.
+ * Only dims->V is read.  Workspace: SPECEE_OP_LOGPROBS with n = N and n_top in the place of Mcap.  N <= 65535.
+ */
+int specee_logprobs(const specee_dims *dims, int N, const float *logits, const specee_half *logits_f16,
+                    long long stride, const int32_t *ids, int T, int n_top, float *logprobs, float *max_logit,
+                    float *log_sum, float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace,
+                    size_t workspace_bytes, void *stream);
+
+/*
+ * Gradient of specee_logprobs: with p = exp(log p(v)) and the gradients g_t of logprobs[n][t] and h of entropy[n],
+ *     grad[n][v] = sum of g_t over all t with ids[n][t] == v  -  p * (sum of all g_t + h * (log p(v) + entropy)).
+ *   logits / logits_f16, stride, ids, T as there (ids may repeat; ids outside [0, V) add nothing), max_logit,
+ *   log_sum [N] as it wrote them, entropy [N] as it wrote it if g_entropy is given.
+ *   g_logprobs [N][T] (NULL if T is 0), g_entropy [N] or NULL.
+ *   grad / grad_f16 of the logits' type, rows grad_stride elements apart; may be the logits themselves with
+ *   their stride, and may not overlap them otherwise.  Elements between rows are left as they are.
+ * A row of -inf alone has gradient 0, a row with a NaN or +inf NaN.  Needs no workspace.  N <= 65535.
+ */
+int specee_logprobs_grad(const specee_dims *dims, int N, const float *logits, const specee_half *logits_f16,
+                         long long stride, const int32_t *ids, int T, const float *max_logit, const float *log_sum,
+                         const float *entropy, const float *g_logprobs, const float *g_entropy, float *grad,
+                         specee_half *grad_f16, long long grad_stride, void *stream);
 
 /* Bytes of device workspace `op` needs for n tokens / nodes (Mcap: tree only).
  * Pure host function; 0 means none; (size_t)-1 means invalid arguments. */

@@ -217,4 +217,38 @@ hipError_t launch_head_states_argmax(int d, int V, float eps, int N, const half_
                                      const half_t *lm_head, const HeadQ4 &q4, int workgroups, float *best_val,
                                      int32_t *best_idx, const int32_t *gate, const int32_t *done, hipStream_t s);
 
+// Norms around a block with its gate and residual scale (block_norm.hip); what may be null is what the header says
+struct BlockNormParams {
+    int N, d, gate_rows;
+    float eps, hidden_scale, branch_scale;
+    const half_t *hidden, *branch, *gamma_post, *gate, *gamma;
+    half_t *hidden_out, *x;
+    uint8_t *x8;
+    float *x8_scales;
+};
+hipError_t launch_block_norm(const BlockNormParams &p, hipStream_t s);
+
+// Log probabilities of rows of logits, fp32 or fp16, and their gradient (logprobs.hip)
+struct LogprobsParams {
+    int N, V, T, K, parts;  // K alternatives; parts: workgroups per row (logprobs_parts)
+    long long stride;
+    const void *logits;
+    const int32_t *ids;  // [N][T]
+    float *logprobs, *max_logit, *log_sum, *entropy, *top_logprobs;
+    int32_t *top_ids;
+    float *part_sums, *part_vals;  // with several parts: [N][parts][4], [N][parts][K]
+    int32_t *part_ids;
+};
+struct LogprobsGradParams {
+    int N, V, T;
+    long long stride, grad_stride;
+    const void *logits;
+    const int32_t *ids;
+    const float *max_logit, *log_sum, *entropy, *g_logprobs, *g_entropy;
+    void *grad;
+};
+int logprobs_parts(int N, int V, bool half);
+hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s);
+hipError_t launch_logprobs_grad(const LogprobsGradParams &p, bool half, hipStream_t s);
+
 }  // namespace specee

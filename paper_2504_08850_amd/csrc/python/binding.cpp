@@ -7,7 +7,7 @@
 //   T *                  the same without a check of the type (outputs); void *: any tensor
 //   const specee_dims *  tuple (d, V, K, H, eps, threshold)
 //   const specee_mlp *   tuple (W1, b1, w2, b2) of fp16 tensors or None
-//   integers             anything with __index__
+//   integers, float      anything with __index__, __float__
 //   last argument        the stream: None (the current one) or its handle
 // The tensors outlive the call: the caller's argument list holds them.
 #define PY_SSIZE_T_CLEAN
@@ -60,6 +60,10 @@ struct Elem<int32_t> {
     static constexpr c10::ScalarType type = c10::ScalarType::Int;
 };
 template <>
+struct Elem<specee_f8> {
+    static constexpr c10::ScalarType type = c10::ScalarType::Float8_e4m3fn;
+};
+template <>
 struct Elem<uint32_t> {  // words travel as int32
     static constexpr c10::ScalarType type = c10::ScalarType::Int;
 };
@@ -99,6 +103,16 @@ template <>
 struct Arg<long long> : IntArg<long long> {};
 template <>
 struct Arg<size_t> : IntArg<size_t> {};
+
+template <>
+struct Arg<float> {
+    double v;
+    bool from(PyObject *o) {
+        v = PyFloat_AsDouble(o);
+        return !(v == -1.0 && PyErr_Occurred());
+    }
+    float get() { return static_cast<float>(v); }
+};
 
 bool tuple_of(PyObject *o, Py_ssize_t n) {
     if (PyTuple_Check(o) && PyTuple_GET_SIZE(o) == n) return true;
@@ -196,6 +210,8 @@ PyMethodDef methods[] = {
     SPECEE_ENTRY(lm_head_gemv),          SPECEE_ENTRY(lm_head_gemv_q4),
     SPECEE_ENTRY(specee_verify),         SPECEE_ENTRY(specee_verify_q4),
     SPECEE_ENTRY(specee_layer_loop),     SPECEE_ENTRY(specee_layer_loop_q4),
+    SPECEE_ENTRY(specee_block_norm),     SPECEE_ENTRY(specee_logprobs),
+    SPECEE_ENTRY(specee_logprobs_grad),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of libspecee.so", -1, methods,

@@ -127,6 +127,27 @@ size_t whole_tree_bytes(int G, int S, int Mcap) {
     return whole_tree_part_bytes(G, S, Mcap) + whole_tree_ssq_bytes(G, S) + align256((size_t)G * sizeof(int32_t));
 }
 
+// Workspace of specee_logprobs: what the parts of a row leave for the launch that joins them
+struct LogprobsLayout {
+    size_t vals_off, ids_off, total;
+};
+LogprobsLayout logprobs_layout(int N, int parts, int K) {
+    LogprobsLayout l{0, 0, 0};
+    if (parts < 2) return l;
+    const size_t n = (size_t)N * parts;
+    l.vals_off = align256(n * 4 * sizeof(float));
+    l.ids_off = l.vals_off + align256(n * K * sizeof(float));
+    l.total = l.ids_off + align256(n * K * sizeof(int32_t));
+    return l;
+}
+int check_logits(const specee_dims *dm, int N, const void *logits, const void *logits_f16, long long stride, int T) {
+    if (!dm || dm->V < 1 || N < 0 || N > 65535 || T < 0 || T > SPECEE_IDS_MAX) return SPECEE_EINVAL;
+    if (N == 0) return SPECEE_OK;
+    if (!logits == !logits_f16 || stride < dm->V || stride > (1ll << 40)) return SPECEE_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(logits) & 3) || (reinterpret_cast<uintptr_t>(logits_f16) & 1)) return SPECEE_EALIGN;
+    return SPECEE_OK;
+}
+
 }  // namespace
 
 // Scratch memory of specee_predict_tree_static, the entry point for callers that cannot allocate.
@@ -198,6 +219,9 @@ size_t specee_workspace_bytes(int op, const specee_dims *dm, int n, int Mcap) {
                                             n >= 2 && dm->d % 64 == 0
                                                 ? head_states_workgroups(dm->d, dm->V, dm->d % 128 == 0 ? 128 : 64, INT_MAX)
                                                 : 0));
+        case SPECEE_OP_LOGPROBS:  // (fp16 rows are cut into no more parts than fp32 rows)
+            if (!dm || dm->V < 1 || n > 65535 || Mcap < 0 || Mcap > SPECEE_TOP_MAX) return (size_t)-1;
+            return logprobs_layout(n, logprobs_parts(n, dm->V, false), Mcap).total;
         case SPECEE_OP_LAYER_LOOP:
             if (check_dims(dm, true) || n > kLoopMaxTokens) return (size_t)-1;
             return loop_layout(n).total;
@@ -653,6 +677,80 @@ int specee_layer_loop_q4(const specee_dims *dm, int L, int B, const specee_half 
     return layer_loop_common(dm, L, B, hidden, gamma, nullptr, qweight, scales, zeros, group, ids, prev0, mlp, active,
                              logits, probs, scores, exit_flags, ver_token, hit, exit_layer, token, status, spin_limit,
                              workspace, workspace_bytes, stream, true);
+}
+
+int specee_block_norm(const specee_dims *dm, int N, const specee_half *hidden, const specee_half *branch,
+                      const specee_half *gamma_post, const specee_half *gate, int gate_rows, float hidden_scale,
+                      float branch_scale, const specee_half *gamma, specee_half *hidden_out, specee_half *x,
+                      specee_f8 *x8, float *x8_scales, void *stream) {
+    if (!dm || dm->d < 8 || (dm->d & 7) || dm->d > 16384 || !(dm->eps >= 0.f) || N < 0 || N > (1 << 22))
+        return SPECEE_EINVAL;
+    if (N == 0) return SPECEE_OK;
+    if (!hidden || !x8 != !x8_scales || (!gamma && (x || x8)) || (!hidden_out && !x && !x8)) return SPECEE_EINVAL;
+    if (!branch && (gamma_post || gate)) return SPECEE_EINVAL;
+    if (gate && gate_rows != 1 && gate_rows != N) return SPECEE_EINVAL;
+    if (x && x == hidden_out) return SPECEE_EINVAL;
+    if (misaligned(hidden) || misaligned(branch) || misaligned(gamma_post) || misaligned(gate) || misaligned(gamma) ||
+        misaligned(hidden_out) || misaligned(x) || misaligned(x8))
+        return SPECEE_EALIGN;
+    BlockNormParams p{};
+    p.N = N; p.d = dm->d; p.gate_rows = gate_rows;
+    p.eps = dm->eps; p.hidden_scale = hidden_scale; p.branch_scale = branch_scale;
+    p.hidden = H(hidden); p.branch = H(branch); p.gamma_post = H(gamma_post); p.gate = H(gate); p.gamma = H(gamma);
+    p.hidden_out = reinterpret_cast<half_t *>(hidden_out); p.x = reinterpret_cast<half_t *>(x);
+    p.x8 = x8; p.x8_scales = x8_scales;
+    return launch_block_norm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEE_OK : SPECEE_EHIP;
+}
+
+int specee_logprobs(const specee_dims *dm, int N, const float *logits, const specee_half *logits_f16, long long stride,
+                    const int32_t *ids, int T, int n_top, float *logprobs, float *max_logit, float *log_sum,
+                    float *entropy, int32_t *top_ids, float *top_logprobs, void *workspace, size_t workspace_bytes,
+                    void *stream) {
+    int rc = check_logits(dm, N, logits, logits_f16, stride, T);
+    if (rc) return rc;
+    if (n_top < 0 || n_top > SPECEE_TOP_MAX) return SPECEE_EINVAL;
+    if (N == 0) return SPECEE_OK;
+    if ((T > 0 && (!ids || !logprobs)) || (n_top > 0 && (!top_ids || !top_logprobs))) return SPECEE_EINVAL;
+    LogprobsParams p{};
+    p.N = N; p.V = dm->V; p.T = T; p.K = n_top; p.stride = stride;
+    p.parts = logprobs_parts(N, dm->V, logits_f16 != nullptr);
+    p.logits = logits ? static_cast<const void *>(logits) : logits_f16;
+    p.ids = ids; p.logprobs = logprobs; p.max_logit = max_logit; p.log_sum = log_sum; p.entropy = entropy;
+    p.top_ids = top_ids; p.top_logprobs = top_logprobs;
+    const LogprobsLayout lay = logprobs_layout(N, p.parts, n_top);
+    if (lay.total) {
+        if (misaligned(workspace)) return SPECEE_EALIGN;
+        if (!workspace || workspace_bytes < lay.total) return SPECEE_EWORKSPACE;
+        char *ws = static_cast<char *>(workspace);
+        p.part_sums = reinterpret_cast<float *>(ws);
+        p.part_vals = reinterpret_cast<float *>(ws + lay.vals_off);
+        p.part_ids = reinterpret_cast<int32_t *>(ws + lay.ids_off);
+    }
+    return launch_logprobs(p, logits_f16 != nullptr, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEE_OK
+                                                                                                     : SPECEE_EHIP;
+}
+
+int specee_logprobs_grad(const specee_dims *dm, int N, const float *logits, const specee_half *logits_f16,
+                         long long stride, const int32_t *ids, int T, const float *max_logit, const float *log_sum,
+                         const float *entropy, const float *g_logprobs, const float *g_entropy, float *grad,
+                         specee_half *grad_f16, long long grad_stride, void *stream) {
+    int rc = check_logits(dm, N, logits, logits_f16, stride, T);
+    if (rc) return rc;
+    if (N == 0) return SPECEE_OK;
+    if ((T > 0 && (!ids || !g_logprobs)) || !max_logit || !log_sum || (g_entropy && !entropy)) return SPECEE_EINVAL;
+    if ((logits ? !grad : !grad_f16) || (grad && grad_f16)) return SPECEE_EINVAL;
+    if (grad_stride < dm->V || grad_stride > (1ll << 40)) return SPECEE_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(grad) & 3) || (reinterpret_cast<uintptr_t>(grad_f16) & 1)) return SPECEE_EALIGN;
+    LogprobsGradParams p{};
+    p.N = N; p.V = dm->V; p.T = T; p.stride = stride; p.grad_stride = grad_stride;
+    p.logits = logits ? static_cast<const void *>(logits) : logits_f16;
+    p.grad = logits ? static_cast<void *>(grad) : grad_f16;
+    // in place only as a whole: an element is read and written by the same thread
+    if (N > 1 && p.grad == p.logits && grad_stride != stride) return SPECEE_EINVAL;
+    p.ids = ids; p.max_logit = max_logit; p.log_sum = log_sum; p.entropy = entropy;
+    p.g_logprobs = g_logprobs; p.g_entropy = g_entropy;
+    return launch_logprobs_grad(p, logits_f16 != nullptr, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEE_OK
+                                                                                                          : SPECEE_EHIP;
 }
 
 int specee_verify(const specee_dims *dm, int N, const specee_half *hidden, const specee_half *gamma,

@@ -19,7 +19,7 @@ _binding = None
 _REBUILD = "build it with `python -m paper_2504_08850_amd.build` (it takes g++ and torch's headers beside hipcc)"
 
 OP_PREDICT, OP_PREDICT_SWEEP, OP_PREDICT_TREE, OP_LM_HEAD, OP_VERIFY, OP_LAYER_LOOP, OP_VERIFY_Q4, \
-    OP_PREDICT_TREE_Q4 = range(8)
+    OP_PREDICT_TREE_Q4, OP_LOGPROBS, OP_MATMUL_F8 = range(10)
 
 
 class SpeceeError(RuntimeError):
@@ -404,6 +404,122 @@ def predict_tree_q4(hidden, gamma, qweight, scales, zeros, group, ids, prev_prob
         raise SpeceeError("specee_predict_tree_q4", rc)
     if single:
         return {k: (v[0] if v is not None else None) for k, v in out.items()}
+    return out
+
+
+def _here(t):
+    """The library launches on the current device: a tensor of another one is refused."""
+    assert t.is_cuda, "device-resident tensors only"
+    assert t.get_device() == torch.cuda.current_device(), "the tensors' device has to be the current one"
+    return t.device
+
+
+def block_norm(hidden, gamma=None, branch=None, gamma_post=None, gate=None, hidden_scale=1.0, branch_scale=1.0, eps=1e-5,
+               want_x=True, want_f8=False, out=None, stream=None):
+    """specee_block_norm: hidden_scale * hidden + branch_scale * gate * RMSNorm(branch, gamma_post), and its RMSNorm with
+    gamma.  gate [d] or [1][d] (all rows) or [N][d].  Returns dict(hidden) with x (fp16) if want_x, x8 (float8_e4m3fn)
+    and x8_scales [N][ceil(d/128)] if want_f8; out: such a dict, whose hidden may be `hidden` itself."""
+    N, d = hidden.shape
+    dev = _here(hidden)
+    if gamma is None:
+        want_x = want_f8 = False
+    gate_rows = 0
+    if gate is not None:
+        gate_rows = 1 if gate.dim() == 1 else gate.shape[0]
+        assert gate.shape[-1] == d and gate_rows in (1, N), (gate.shape, hidden.shape)
+    assert branch is None or branch.shape == hidden.shape, (branch.shape, hidden.shape)
+    assert all(g is None or g.shape == (d,) for g in (gamma, gamma_post)), "norm weights are [d]"
+    if out is None:
+        out = dict(hidden=torch.empty_like(hidden))
+        if want_x:
+            out["x"] = torch.empty_like(hidden)
+        if want_f8:
+            out["x8"] = torch.empty((N, d), dtype=torch.float8_e4m3fn, device=dev)
+            out["x8_scales"] = torch.empty((N, (d + 127) // 128), dtype=torch.float32, device=dev)
+    x, x8, scales = (out["x"] if want_x else None), None, None
+    if want_f8:
+        x8, scales = out["x8"], out["x8_scales"]
+        assert x8.dtype == torch.float8_e4m3fn and x8.shape == (N, d), (x8.dtype, x8.shape)
+        assert scales.dtype == torch.float32 and scales.shape == (N, (d + 127) // 128), (scales.dtype, scales.shape)
+    for t in (out["hidden"], x):
+        assert t is None or (t.dtype == torch.float16 and t.shape == hidden.shape), (t.dtype, t.shape)
+    rc = _call().specee_block_norm((d, 1, 1, 1, eps, 0.5), N, hidden, branch, gamma_post, gate, gate_rows, hidden_scale,
+                                   branch_scale, gamma, out["hidden"], x, x8, scales, _handle(stream))
+    if rc:
+        raise SpeceeError("specee_block_norm", rc)
+    return out
+
+
+def _rows(t):
+    """(flat view, stride) of rows of which each is contiguous; the view reaches from the first to the last element."""
+    N, V = t.shape
+    if t.is_contiguous():
+        return t, V
+    assert t.stride(1) == 1 or V == 1, "the elements of a row have to be contiguous"
+    stride = t.stride(0) if N > 1 else V
+    assert stride >= V, "rows that overlap"
+    return t.as_strided(((N - 1) * stride + V,), (1,)), stride
+
+
+def _logits(t):
+    """(fp32, fp16, stride): one of the two is the logits' rows, the other None."""
+    flat, stride = _rows(t)
+    assert t.dtype in (torch.float32, torch.float16), t.dtype
+    return (flat, None, stride) if t.dtype == torch.float32 else (None, flat, stride)
+
+
+def logprobs(logits, ids=None, n_top=0, out=None, workspace=None, stream=None):
+    """specee_logprobs: logits [N][V] fp32 or fp16 (rows may be apart), ids [N][T].  Returns dict(max_logit, log_sum,
+    entropy) with logprobs [N][T] if ids are given, top_ids and top_logprobs [N][n_top] if n_top."""
+    N, V = logits.shape
+    dev = _here(logits)
+    f32, f16, stride = _logits(logits)
+    T = 0 if ids is None else ids.shape[1]
+    assert ids is None or ids.shape[0] == N, (ids.shape, logits.shape)
+    if out is None:
+        new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)
+        out = dict(max_logit=new(N), log_sum=new(N), entropy=new(N))
+        if T:
+            out["logprobs"] = new(N, T)
+        if n_top:
+            out["top_ids"] = torch.empty((N, n_top), dtype=torch.int32, device=dev)
+            out["top_logprobs"] = new(N, n_top)
+    for k, shape in (("max_logit", (N,)), ("log_sum", (N,)), ("entropy", (N,)), ("logprobs", (N, T)),
+                     ("top_logprobs", (N, n_top))):
+        if shape[-1] or N == 0:
+            t = out.get(k) if k in ("max_logit", "log_sum", "entropy") else out[k] if shape[-1] else None
+            assert t is None or (t.dtype == torch.float32 and t.shape == shape), (k, t.dtype, t.shape)
+    dims = (8, V, 1, 1, 0.0, 0.5)
+    workspace, wbytes = _workspace(OP_LOGPROBS, dims, N, n_top, workspace, dev)
+    top_ids = out["top_ids"] if n_top else None
+    assert top_ids is None or (top_ids.dtype == torch.int32 and top_ids.shape == (N, n_top)), top_ids.shape
+    rc = _call().specee_logprobs(dims, N, f32, f16, stride, ids if T else None, T, n_top, out["logprobs"] if T else None,
+                                 out.get("max_logit"), out.get("log_sum"), out.get("entropy"), top_ids,
+                                 out["top_logprobs"] if n_top else None, workspace, wbytes, _handle(stream))
+    if rc:
+        raise SpeceeError("specee_logprobs", rc)
+    out["_workspace"] = workspace
+    return out
+
+
+def logprobs_grad(logits, ids, max_logit, log_sum, entropy=None, g_logprobs=None, g_entropy=None, out=None, stream=None):
+    """specee_logprobs_grad: gradient of the logits of `logprobs`, whose max_logit, log_sum (and entropy, with g_entropy)
+    are given, from those of its log probabilities [N][T] and entropies [N].  `out` may be the logits themselves."""
+    N, V = logits.shape
+    _here(logits)
+    f32, f16, stride = _logits(logits)
+    T = 0 if ids is None else ids.shape[1]
+    assert ids is None or (ids.shape[0] == N and g_logprobs is not None and g_logprobs.shape == ids.shape), "g_logprobs"
+    assert all(t is None or t.shape == (N,) for t in (max_logit, log_sum, entropy, g_entropy)), "one value per row"
+    if out is None:
+        out = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    assert out.dtype == logits.dtype and out.shape == logits.shape, (out.dtype, out.shape)
+    g32, g16, gstride = _logits(out)
+    rc = _call().specee_logprobs_grad((8, V, 1, 1, 0.0, 0.5), N, f32, f16, stride, ids if T else None, T, max_logit,
+                                      log_sum, entropy, g_logprobs if T else None, g_entropy, g32, g16, gstride,
+                                      _handle(stream))
+    if rc:
+        raise SpeceeError("specee_logprobs_grad", rc)
     return out
 
 
