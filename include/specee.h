@@ -368,6 +368,22 @@ int specee_block_norm(const specee_dims *dims, int N, const specee_half *hidden,
                       specee_f8 *x8, float *x8_scales, void *stream);
 
 /*
+ * Matrix product in 8-bit floating point, both sides with a scale for each block of 128: an LM head, or any
+ * projection, kept in e4m3 with one scale per 128 rows by 128 elements, and states as specee_block_norm leaves them,
+ *     out[n][v] = sum over b of x_scales[n][b] * w_scales[v/128][b] * (sum over i in block b of x[n][i] * weight[v][i]).
+ *   x [N][d], x_scales [N][ceil(d/128)]; weight [V][d] (row v = output v), w_scales [ceil(V/128)][ceil(d/128)]; blocks at
+ *   the end may be shorter.  out, out_f16 [N][V]: one of them, the other NULL.
+ * Products and sums are fp32.  For an fp32 result they are formed from the codes as halves, exactly; for an fp16 result
+ * from the codes on the 8-bit matrix cores, which line products of 128 elements up with the largest of them: off by 2e-5 to
+ * 5e-5 of a sum, a twentieth or less of the rounding of the result.
+ * d: a multiple of 16, at most 65536; only dims->d and dims->V are read.
+ * Workspace: SPECEE_OP_MATMUL_F8 with n = N.
+ */
+int specee_matmul_f8(const specee_dims *dims, int N, const specee_f8 *x, const float *x_scales, const specee_f8 *weight,
+                     const float *w_scales, float *out, specee_half *out_f16, void *workspace, size_t workspace_bytes,
+                     void *stream);
+
+/*
  * What is answered with rows of logits (of lm_head_gemv, lm_head_gemv_q4, specee_matmul_f8): the log
  * probabilities of given tokens, the entropy, the best alternatives.  For each row, with m its largest logit
  * and S = sum exp(x - m):

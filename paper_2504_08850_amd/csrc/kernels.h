@@ -228,6 +228,17 @@ struct BlockNormParams {
 };
 hipError_t launch_block_norm(const BlockNormParams &p, hipStream_t s);
 
+// Product in 8-bit floating point with a scale per block of 128 (matmul_f8.hip)
+struct MatmulF8Params {
+    int N, V, d, blocks;  // blocks = ceil(d / 128)
+    const uint8_t *x, *w;  // [N][d], [V][d]
+    const float *xs, *ws;  // [N][blocks], [ceil(V / 128)][blocks]
+    void *out;             // [N][V] fp32 or fp16
+    void *workspace;
+};
+size_t matmul_f8_workspace(int N, int V, int d);
+hipError_t launch_matmul_f8(const MatmulF8Params &p, bool half, hipStream_t s);
+
 // Log probabilities of rows of logits, fp32 or fp16, and their gradient (logprobs.hip)
 struct LogprobsParams {
     int N, V, T, K, parts;  // K alternatives; parts: workgroups per row (logprobs_parts)

@@ -211,7 +211,7 @@ PyMethodDef methods[] = {
     SPECEE_ENTRY(specee_verify),         SPECEE_ENTRY(specee_verify_q4),
     SPECEE_ENTRY(specee_layer_loop),     SPECEE_ENTRY(specee_layer_loop_q4),
     SPECEE_ENTRY(specee_block_norm),     SPECEE_ENTRY(specee_logprobs),
-    SPECEE_ENTRY(specee_logprobs_grad),
+    SPECEE_ENTRY(specee_logprobs_grad),  SPECEE_ENTRY(specee_matmul_f8),
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of libspecee.so", -1, methods,

@@ -140,6 +140,11 @@ LogprobsLayout logprobs_layout(int N, int parts, int K) {
     l.total = l.ids_off + align256(n * K * sizeof(int32_t));
     return l;
 }
+int check_f8(const specee_dims *dm, int N) {
+    if (!dm || dm->d < 16 || (dm->d & 15) || dm->d > 65536 || dm->V < 1 || dm->V > (1 << 24) || N < 0 || N > (1 << 22))
+        return SPECEE_EINVAL;
+    return SPECEE_OK;
+}
 int check_logits(const specee_dims *dm, int N, const void *logits, const void *logits_f16, long long stride, int T) {
     if (!dm || dm->V < 1 || N < 0 || N > 65535 || T < 0 || T > SPECEE_IDS_MAX) return SPECEE_EINVAL;
     if (N == 0) return SPECEE_OK;
@@ -219,6 +224,8 @@ size_t specee_workspace_bytes(int op, const specee_dims *dm, int n, int Mcap) {
                                             n >= 2 && dm->d % 64 == 0
                                                 ? head_states_workgroups(dm->d, dm->V, dm->d % 128 == 0 ? 128 : 64, INT_MAX)
                                                 : 0));
+        case SPECEE_OP_MATMUL_F8:
+            return check_f8(dm, n) ? (size_t)-1 : matmul_f8_workspace(n, dm->V, dm->d);
         case SPECEE_OP_LOGPROBS:  // (fp16 rows are cut into no more parts than fp32 rows)
             if (!dm || dm->V < 1 || n > 65535 || Mcap < 0 || Mcap > SPECEE_TOP_MAX) return (size_t)-1;
             return logprobs_layout(n, logprobs_parts(n, dm->V, false), Mcap).total;
@@ -700,6 +707,26 @@ int specee_block_norm(const specee_dims *dm, int N, const specee_half *hidden, c
     p.hidden_out = reinterpret_cast<half_t *>(hidden_out); p.x = reinterpret_cast<half_t *>(x);
     p.x8 = x8; p.x8_scales = x8_scales;
     return launch_block_norm(p, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEE_OK : SPECEE_EHIP;
+}
+
+int specee_matmul_f8(const specee_dims *dm, int N, const specee_f8 *x, const float *x_scales, const specee_f8 *weight,
+                     const float *w_scales, float *out, specee_half *out_f16, void *workspace, size_t workspace_bytes,
+                     void *stream) {
+    int rc = check_f8(dm, N);
+    if (rc) return rc;
+    if (N == 0) return SPECEE_OK;
+    if (!x || !x_scales || !weight || !w_scales || !out == !out_f16) return SPECEE_EINVAL;
+    if (misaligned(x) || misaligned(weight) || misaligned(out) || misaligned(out_f16) || misaligned(workspace))
+        return SPECEE_EALIGN;
+    const size_t need = matmul_f8_workspace(N, dm->V, dm->d);
+    if (need && (!workspace || workspace_bytes < need)) return SPECEE_EWORKSPACE;
+    MatmulF8Params p{};
+    p.N = N; p.V = dm->V; p.d = dm->d; p.blocks = (dm->d + 127) / 128;
+    p.x = x; p.xs = x_scales; p.w = weight; p.ws = w_scales;
+    p.out = out ? static_cast<void *>(out) : out_f16;
+    p.workspace = workspace;
+    return launch_matmul_f8(p, out_f16 != nullptr, static_cast<hipStream_t>(stream)) == hipSuccess ? SPECEE_OK
+                                                                                                   : SPECEE_EHIP;
 }
 
 int specee_logprobs(const specee_dims *dm, int N, const float *logits, const specee_half *logits_f16, long long stride,

@@ -450,6 +450,27 @@ def block_norm(hidden, gamma=None, branch=None, gamma_post=None, gate=None, hidd
     return out
 
 
+def matmul_f8(x, x_scales, weight, w_scales, dtype=torch.float32, out=None, workspace=None, stream=None):
+    """specee_matmul_f8: x [N][d] and weight [V][d] float8_e4m3fn, x_scales [N][ceil(d/128)] and w_scales
+    [ceil(V/128)][ceil(d/128)] fp32; returns dict(out) with out [N][V] of `dtype`, fp32 or fp16."""
+    N, d = x.shape
+    V = weight.shape[0]
+    dev = _here(x)
+    nb = (d + 127) // 128
+    assert weight.shape[1] == d and x_scales.shape == (N, nb) and w_scales.shape == ((V + 127) // 128, nb), \
+        (x.shape, x_scales.shape, weight.shape, w_scales.shape)
+    if out is None:
+        out = torch.empty((N, V), dtype=dtype, device=dev)
+    assert out.dtype in (torch.float32, torch.float16) and out.dtype == dtype and out.shape == (N, V), (out.dtype, out.shape)
+    dims = (d, V, 1, 1, 0.0, 0.5)
+    workspace, wbytes = _workspace(OP_MATMUL_F8, dims, N, 0, workspace, dev)
+    f32, f16 = (out, None) if dtype == torch.float32 else (None, out)
+    rc = _call().specee_matmul_f8(dims, N, x, x_scales, weight, w_scales, f32, f16, workspace, wbytes, _handle(stream))
+    if rc:
+        raise SpeceeError("specee_matmul_f8", rc)
+    return dict(out=out, _workspace=workspace)
+
+
 def _rows(t):
     """(flat view, stride) of rows of which each is contiguous; the view reaches from the first to the last element."""
     N, V = t.shape

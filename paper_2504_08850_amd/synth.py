@@ -63,6 +63,30 @@ def quantize_q4(w: np.ndarray, group: int = 128, chunk_rows: int = 2048):
     return q, scales, zeros
 
 
+def e4m3(v: np.ndarray) -> np.ndarray:
+    """Codes (uint8) of the e4m3 numbers nearest to v, ties to even; |v| up to 464 (what lies above 448 becomes 448)."""
+    a = np.minimum(np.abs(v.astype(np.float64)), 448.0)
+    exponent = np.maximum(np.floor(np.log2(np.maximum(a, 2.0 ** -60))), -6)      # below 2^-6 the steps stay 2^-9
+    step = np.rint(a * 2.0 ** (3 - exponent))                                    # 8..16, or 0..8 below the normal numbers
+    code = np.where(step < 8, step, (exponent + 7) * 8 + step - 8)               # (a step of 16 is the next exponent's 8)
+    return (code.astype(np.uint8) | np.where(np.signbit(v), 128, 0).astype(np.uint8))
+
+
+def quantize_f8(w: np.ndarray, rows: int = 128):
+    """8-bit copy of a matrix [V][d], the storage that specee_matmul_f8 reads: e4m3 codes (uint8 [V][d]) and one fp32 scale
+    for every `rows` rows by 128 elements ([ceil(V/rows)][ceil(d/128)]; weights rows = 128, states rows = 1): the largest
+    absolute value of the block / 448, 1 where all of it is 0."""
+    V, d = w.shape
+    nv, nb = -(-V // rows), -(-d // 128)
+    pad = np.zeros((nv * rows, nb * 128), dtype=np.float32)
+    pad[:V, :d] = w
+    blk = pad.reshape(nv, rows, nb, 128)
+    top = np.abs(blk).max(axis=(1, 3))
+    scales = np.where(top > 0, top / np.float32(448.0), np.float32(1.0)).astype(np.float32)
+    codes = e4m3(blk / scales[:, None, :, None]).reshape(nv * rows, nb * 128)[:V, :d]
+    return np.ascontiguousarray(codes), scales
+
+
 def gamma(d: int, seed: int) -> np.ndarray:
     return (1.0 + 0.01 * _rng(seed, 2).standard_normal(d)).astype(np.float16)
 
