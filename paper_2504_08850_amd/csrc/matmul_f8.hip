@@ -1,5 +1,7 @@
 // Matrix product in 8-bit floating point (e4m3) with a scale for each block of 128:
 //     out[n][v] = sum over b of xs[n][b] * ws[v / 128][b] * (sum over i in block b of x[n][i] * w[v][i]).
+#include <limits.h>
+
 #include <type_traits>
 
 #include "../../include/specee.h"
@@ -19,11 +21,13 @@ constexpr int kOne = 0x7f7f7f7f;  // block scales of 2^0 for the matrix instruct
 union Codes {
     uintx4 piece[2];
     intx8 all;
+    __device__ __forceinline__ Codes() {}
 };
 
 // The codes as halves (exact), eight to a register group
 struct Halves {
     half8 part[4];
+    __device__ __forceinline__ Halves() {}
     __device__ __forceinline__ explicit Halves(const Codes &c) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -63,95 +67,231 @@ __device__ __forceinline__ void store_quad(T *out, size_t at, int left, const fl
     }
 }
 
-constexpr int kTile = 128;  // rows of w and of x per workgroup
+// 16 (4) bytes per lane from base + off to LDS at lds + 16 (4) * lane, without a stop in registers.  The compiler does not
+// count these loads (with its own builtin it waits for all of them before any read of LDS): landed<n>() waits for all but the
+// last n of them.
+__device__ __forceinline__ void load_lds16(uint32_t lds, uint32_t off, const void *base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void load_lds4(uint32_t lds, uint32_t off, const void *base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
+// ... and for the wavefront's LDS traffic, then meets the workgroup
+template <int N>
+__device__ __forceinline__ void landed() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// A workgroup's tile: WV wavefronts of 128 rows of w by 4 of NJ * 16 rows of x
+template <int WV, int NJ>
+struct Tile {
+    static constexpr int waves = WV * 4, threads = waves * kWave;
+    static constexpr int rows = WV * 128, states = NJ * 64;
+    static constexpr int w_bytes = rows * kBlock, x_bytes = states * kBlock;
+    static constexpr int buffer = w_bytes + x_bytes + states * 4;  // of one block
+    static constexpr int buffers = 3 * buffer <= 156 * 1024 ? 3 : 2;
+    static constexpr int w_loads = rows / 8 / waves, x_loads = states / 8 / waves;  // of a wavefront, 8 rows each
+    static constexpr int loads = w_loads + x_loads + 1;
+};
 
 // T: type of the result.  fp16 results take the codes as they are, fp32 results as halves.
-template <typename T>
-__global__ __launch_bounds__(256) void matmul_f8_kernel(MatmulF8Params p) {
+template <typename T, int WV, int NJ>
+__global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p) {
+    using S = Tile<WV, NJ>;
     constexpr bool kExact = sizeof(T) == 4;
     typedef typename std::conditional<kExact, Halves, Codes>::type Operand;
-    __shared__ uintx4 wt[2][kTile * 8], xt[2][kTile * 8];
-    __shared__ float st[2][kTile];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, q = lane >> 4, c = lane & 15;
-    const int v0 = blockIdx.x * kTile, n0 = blockIdx.y * kTile;
-    const int wv = (wave & 1) * 64, wn = (wave >> 1) * 64;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char f8_smem[];
+    const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wv = wave >> 2, wn = wave & 3;
+    const int v0 = blockIdx.x * S::rows, n0 = blockIdx.y * S::states;
+    const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
+    const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
 
-    uintx4 wr[4], xr[4];
-    float sr = 0.f;
+    // A load brings eight rows of a tile, a row's eight pieces of 16 bytes in the order piece ^ (row % 8): the 16 rows that
+    // the lanes of an operand read then lie in different banks
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)f8_smem;
+    const int sub = lane >> 3, piece = ((lane & 7) ^ sub) * 16;
+    const uint8_t *wbase = p.w + (size_t)v0 * p.d, *xbase = p.x + (size_t)n0 * p.d;
+    uint32_t woff[S::w_loads], xoff[S::x_loads];
+#pragma unroll
+    for (int i = 0; i < S::w_loads; ++i)
+        woff[i] = (uint32_t)min((wave * S::w_loads + i) * 8 + sub, p.V - 1 - v0) * (uint32_t)p.d + piece;
+#pragma unroll
+    for (int i = 0; i < S::x_loads; ++i)
+        xoff[i] = (uint32_t)min((wave * S::x_loads + i) * 8 + sub, p.N - 1 - n0) * (uint32_t)p.d + piece;
+    const int sn = (wave % NJ) * 64 + lane;  // (a scale is loaded by every wavefront that has nothing else to load)
+    const float *sbase = p.xs + (size_t)n0 * p.blocks;
+    const uint32_t soff = (uint32_t)min(sn, p.N - 1 - n0) * (uint32_t)p.blocks * 4;
+
     auto load = [&](int b) {
+        const int slot = (b - b0) % S::buffers;
+        const uint32_t at = lds0 + slot * S::buffer;
+        const int k0 = b * kBlock;
+        if (k0 + kBlock <= p.d) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = (tid >> 3) + i * 32, k = b * kBlock + (tid & 7) * 16;
-            const bool in = k < p.d;
-            const int ks = in ? k : 0;
-            wr[i] = *reinterpret_cast<const uintx4 *>(p.w + (size_t)min(v0 + r, p.V - 1) * p.d + ks);
-            xr[i] = *reinterpret_cast<const uintx4 *>(p.x + (size_t)min(n0 + r, p.N - 1) * p.d + ks);
-            if (!in) wr[i] = xr[i] = uintx4{0, 0, 0, 0};
-        }
-        if (tid < kTile) sr = p.xs[(size_t)min(n0 + tid, p.N - 1) * p.blocks + b] * p.ws[(size_t)blockIdx.x * p.blocks + b];
-    };
-    auto keep = [&](int buf) {
+            for (int i = 0; i < S::w_loads; ++i) load_lds16(at + (wave * S::w_loads + i) * 1024, woff[i], wbase + k0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = (tid >> 3) + i * 32, at = r * 8 + ((tid & 7) ^ (r & 7));
-            wt[buf][at] = wr[i];
-            xt[buf][at] = xr[i];
-        }
-        if (tid < kTile) st[buf][tid] = sr;
-    };
-    auto operand = [&](const uintx4 *t, int r) {
-        Codes o;
-        o.piece[0] = t[r * 8 + (q ^ (r & 7))];
-        o.piece[1] = t[r * 8 + ((q + 4) ^ (r & 7))];
-        return o;
-    };
-
-    floatx4 acc[4][4] = {};
-    load(0);
-    keep(0);
-    __syncthreads();
-    for (int b = 0; b < p.blocks; ++b) {
-        const int buf = b & 1;
-        if (b + 1 < p.blocks) load(b + 1);
+            for (int i = 0; i < S::x_loads; ++i)
+                load_lds16(at + S::w_bytes + (wave * S::x_loads + i) * 1024, xoff[i], xbase + k0);
+        } else {  // a last block that is shorter: zeros behind the rows' ends
+            const bool in = k0 + piece < p.d;
+            uintx4 *dst = reinterpret_cast<uintx4 *>(f8_smem + slot * S::buffer) + lane;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const Operand x(operand(xt[buf], wn + j * 16 + c));
-            const float s = st[buf][wn + j * 16 + c];
+            for (int i = 0; i < S::w_loads; ++i) {
+                uintx4 v = *reinterpret_cast<const uintx4 *>(wbase + (in ? k0 + woff[i] : 0u));
+                if (!in) v = uintx4{0, 0, 0, 0};
+                dst[(wave * S::w_loads + i) * 64] = v;
+            }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const floatx4 t = block_product(Operand(operand(wt[buf], wv + i * 16 + c)), x);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s, t[e], acc[i][j][e]);
+            for (int i = 0; i < S::x_loads; ++i) {
+                uintx4 v = *reinterpret_cast<const uintx4 *>(xbase + (in ? k0 + xoff[i] : 0u));
+                if (!in) v = uintx4{0, 0, 0, 0};
+                dst[S::w_bytes / 16 + (wave * S::x_loads + i) * 64] = v;
             }
         }
-        if (b + 1 < p.blocks) keep(buf ^ 1);
-        __syncthreads();
-    }
+        load_lds4(at + S::w_bytes + S::x_bytes + (wave % NJ) * 256, soff, sbase + b);
+    };
+
+    floatx4 acc[8][NJ] = {};
+    const int frag = c * kBlock + ((q ^ (c & 7)) << 4);
+    // (a scalar load: a vector load would be waited for behind the tiles that are in flight)
+    typedef const __attribute__((address_space(4))) float *scalar_ptr;
+    const scalar_ptr ws = (scalar_ptr)(uintptr_t)(p.ws + (size_t)min((v0 >> 7) + wv, (p.V - 1) >> 7) * p.blocks);
+    float sw = ws[b0];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + wn + j * 16 + c;
+    for (int k = 0; k < S::buffers - 1; ++k)
+        if (b0 + k < b1) load(b0 + k);
+    for (int b = b0; b < b1; ++b) {
+        if (S::buffers == 3 && b + 1 < b1)
+            landed<S::loads>();
+        else
+            landed<0>();
+        if (b + S::buffers - 1 < b1) load(b + S::buffers - 1);
+        const float sw_next = ws[min(b + 1, b1 - 1)];
+        const unsigned char *buf = f8_smem + ((b - b0) % S::buffers) * S::buffer;
+        const unsigned char *wt = buf + wv * 128 * kBlock, *xt = buf + S::w_bytes + wn * NJ * 16 * kBlock;
+        const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * NJ * 16 + c;
+        auto operand = [&](const unsigned char *t, int i) {
+            Codes o;
+            o.piece[0] = *reinterpret_cast<const uintx4 *>(t + i * 16 * kBlock + frag);
+            o.piece[1] = *reinterpret_cast<const uintx4 *>(t + i * 16 * kBlock + (frag ^ 64));
+            return Operand(o);
+        };
+        float s[NJ];
+        Operand x[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            x[j] = operand(xt, j);
+            s[j] = st[j * 16] * sw;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const Operand w = operand(wt, i);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const floatx4 t = block_product(w, x[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[j], t[e], acc[i][j][e]);
+            }
+        }
+        sw = sw_next;
+    }
+    const bool parts = gridDim.z > 1;
+    float *part = static_cast<float *>(p.workspace) + (size_t)blockIdx.z * p.N * p.V;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        const int n = n0 + (wn * NJ + j) * 16 + c;
         if (n >= p.N) continue;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int v = v0 + wv + i * 16 + 4 * q;
-            if (v < p.V) store_quad(static_cast<T *>(p.out), (size_t)n * p.V + v, p.V - v, acc[i][j]);
+        for (int i = 0; i < 8; ++i) {
+            const int v = v0 + wv * 128 + i * 16 + 4 * q;
+            if (v >= p.V) continue;
+            if (parts)
+                store_quad(part, (size_t)n * p.V + v, p.V - v, acc[i][j]);
+            else
+                store_quad(static_cast<T *>(p.out), (size_t)n * p.V + v, p.V - v, acc[i][j]);
         }
     }
+}
+
+// Sums of the parts, in their order
+template <typename T>
+__global__ __launch_bounds__(256) void matmul_f8_join_kernel(const float *part, int parts, size_t n, T *out) {
+    const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= n) return;
+    const int left = n - i < 4 ? (int)(n - i) : 4;
+    floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < parts; ++s)
+        for (int e = 0; e < left; ++e) sum[e] += part[(size_t)s * n + i + e];
+    store_quad(out, i, left, sum);
+}
+
+struct Shape {
+    int wv, nj, parts;
+};
+
+Shape shape_of(int N, int V, int d) {
+    const int blocks = (d + kBlock - 1) / kBlock;
+    Shape best{1, (N + 63) / 64 > 4 ? 4 : (N + 63) / 64, 1};
+    if (N > 256) {
+        long cost = LONG_MAX;
+        for (int nj = 2; nj <= 4; ++nj) {
+            const long tiles = (long)((V + 255) / 256) * ((N + 64 * nj - 1) / (64 * nj));
+            const long c = ((tiles + 255) / 256) * (2 * nj + 1);
+            if (c < cost) {
+                cost = c;
+                best = Shape{2, nj, 1};
+            }
+        }
+    }
+    const long tiles = (long)((V + 128 * best.wv - 1) / (128 * best.wv)) * ((N + 64 * best.nj - 1) / (64 * best.nj));
+    while (best.parts < 8 && tiles * best.parts * 2 <= 256 && blocks >= best.parts * 2 * 4) best.parts *= 2;
+    return best;
+}
+
+template <typename T, int WV, int NJ>
+hipError_t launch_tile(const MatmulF8Params &p, int parts, hipStream_t s) {
+    using S = Tile<WV, NJ>;
+    const auto kern = matmul_f8_kernel<T, WV, NJ>;
+    const int lds = S::buffers * S::buffer;
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const dim3 grid((p.V + S::rows - 1) / S::rows, (p.N + S::states - 1) / S::states, parts);
+    hipLaunchKernelGGL(kern, grid, dim3(S::threads), lds, s, p);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s) {
+    hipError_t e;
+    switch (sh.wv * 10 + sh.nj) {
+        case 11: e = launch_tile<T, 1, 1>(p, sh.parts, s); break;
+        case 12: e = launch_tile<T, 1, 2>(p, sh.parts, s); break;
+        case 13: e = launch_tile<T, 1, 3>(p, sh.parts, s); break;
+        case 14: e = launch_tile<T, 1, 4>(p, sh.parts, s); break;
+        case 22: e = launch_tile<T, 2, 2>(p, sh.parts, s); break;
+        case 23: e = launch_tile<T, 2, 3>(p, sh.parts, s); break;
+        case 24: e = launch_tile<T, 2, 4>(p, sh.parts, s); break;
+        default: return hipErrorInvalidValue;
+    }
+    if (e != hipSuccess || sh.parts == 1) return e;
+    const size_t n = (size_t)p.N * p.V;
+    hipLaunchKernelGGL(matmul_f8_join_kernel<T>, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s,
+                       static_cast<const float *>(p.workspace), sh.parts, n, static_cast<T *>(p.out));
+    return hipGetLastError();
 }
 
 }  // namespace
 
 size_t matmul_f8_workspace(int N, int V, int d) {
-    return 0;
+    if (N < 1) return 0;
+    const Shape s = shape_of(N, V, d);
+    return s.parts > 1 ? (size_t)s.parts * N * V * sizeof(float) : 0;
 }
 
 hipError_t launch_matmul_f8(const MatmulF8Params &p, bool half, hipStream_t s) {
-    const dim3 grid((p.V + kTile - 1) / kTile, (p.N + kTile - 1) / kTile);
-    if (half)
-        hipLaunchKernelGGL(matmul_f8_kernel<half_t>, grid, dim3(256), 0, s, p);
-    else
-        hipLaunchKernelGGL(matmul_f8_kernel<float>, grid, dim3(256), 0, s, p);
-    return hipGetLastError();
+    const Shape sh = shape_of(p.N, p.V, p.d);
+    return half ? launch_shape<half_t>(p, sh, s) : launch_shape<float>(p, sh, s);
 }
 
 }  // namespace specee

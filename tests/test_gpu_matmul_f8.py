@@ -235,6 +235,7 @@ def test_refusals_without_a_gpu(sp):
     assert call(out=None) == -1 and call(h=a) == -1
     assert call(x=odd) == -2 and call(w=odd) == -2 and call(out=odd) == -2 and call(wk=odd) == -2
     assert call(N=0, x=None, out=None) == 0
+    assert sp.workspace_bytes(sp.OP_MATMUL_F8, sp.Dims(4096, 4096, 1, 1, 0.0, 0.5), 0) == 0
     with pytest.raises(sp.SpeceeError):
         sp.workspace_bytes(sp.OP_MATMUL_F8, sp.Dims(24, 64, 1, 1, 0.0, 0.5), 1)
 
