@@ -15,7 +15,6 @@ namespace {
 typedef int intx8 __attribute__((ext_vector_type(8)));
 
 constexpr int kBlock = 128;  // elements, or rows of w, that share a scale
-constexpr int kOne = 0x7f7f7f7f;  // block scales of 2^0 for the matrix instruction
 
 // 32 codes of a row on a lane: pieces q and q + 4 of 16 in every block
 union Codes {
@@ -45,7 +44,7 @@ struct Halves {
 
 // Sums of one block for 16 rows of w (quads 4q .. 4q + 3 of the result) and 16 of x (column lane % 16)
 __device__ __forceinline__ floatx4 block_product(const Codes &w, const Codes &x) {
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.all, x.all, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, kOne, 0, kOne);
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w.all, x.all, floatx4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0, 0, 0);
 }
 __device__ __forceinline__ floatx4 block_product(const Halves &w, const Halves &x) {
     floatx4 c = {0.f, 0.f, 0.f, 0.f};
@@ -94,49 +93,47 @@ struct Tile {
     static constexpr int loads = w_loads + x_loads + 1;
 };
 
-// T: type of the result.  fp16 results take the codes as they are, fp32 results as halves.
-template <typename T, int WV, int NJ>
-__global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p) {
+// Brings one block of a workgroup's tile to LDS.  A load brings eight rows, a row's eight pieces of 16 bytes in the order
+// piece ^ (row % 8): the 16 rows that the lanes of an operand read then lie in different banks.
+template <int WV, int NJ>
+struct Loader {
     using S = Tile<WV, NJ>;
-    constexpr bool kExact = sizeof(T) == 4;
-    typedef typename std::conditional<kExact, Halves, Codes>::type Operand;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char f8_smem[];
-    const int tid = threadIdx.x, lane = tid & 63, q = lane >> 4, c = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int wv = wave >> 2, wn = wave & 3;
-    const int v0 = blockIdx.x * S::rows, n0 = blockIdx.y * S::states;
-    const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
-    const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
+    const uint8_t *wbase, *xbase;
+    const float *sbase;
+    uint32_t woff[S::w_loads], xoff[S::x_loads], soff;
+    uint32_t lds0;
+    int d, piece, wave, lane;
+    unsigned char *smem;
 
-    // A load brings eight rows of a tile, a row's eight pieces of 16 bytes in the order piece ^ (row % 8): the 16 rows that
-    // the lanes of an operand read then lie in different banks
-    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)f8_smem;
-    const int sub = lane >> 3, piece = ((lane & 7) ^ sub) * 16;
-    const uint8_t *wbase = p.w + (size_t)v0 * p.d, *xbase = p.x + (size_t)n0 * p.d;
-    uint32_t woff[S::w_loads], xoff[S::x_loads];
+    __device__ __forceinline__ Loader(const MatmulF8Params &p, int v0, int n0, int wave_, int lane_, unsigned char *smem_)
+        : d(p.d), wave(wave_), lane(lane_), smem(smem_) {
+        lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
+        const int sub = lane >> 3;
+        piece = ((lane & 7) ^ sub) * 16;
+        wbase = p.w + (size_t)v0 * p.d;
+        xbase = p.x + (size_t)n0 * p.d;
 #pragma unroll
-    for (int i = 0; i < S::w_loads; ++i)
-        woff[i] = (uint32_t)min((wave * S::w_loads + i) * 8 + sub, p.V - 1 - v0) * (uint32_t)p.d + piece;
+        for (int i = 0; i < S::w_loads; ++i)
+            woff[i] = (uint32_t)min((wave * S::w_loads + i) * 8 + sub, p.V - 1 - v0) * (uint32_t)p.d + piece;
 #pragma unroll
-    for (int i = 0; i < S::x_loads; ++i)
-        xoff[i] = (uint32_t)min((wave * S::x_loads + i) * 8 + sub, p.N - 1 - n0) * (uint32_t)p.d + piece;
-    const int sn = (wave % NJ) * 64 + lane;  // (a scale is loaded by every wavefront that has nothing else to load)
-    const float *sbase = p.xs + (size_t)n0 * p.blocks;
-    const uint32_t soff = (uint32_t)min(sn, p.N - 1 - n0) * (uint32_t)p.blocks * 4;
-
-    auto load = [&](int b) {
-        const int slot = (b - b0) % S::buffers;
+        for (int i = 0; i < S::x_loads; ++i)
+            xoff[i] = (uint32_t)min((wave * S::x_loads + i) * 8 + sub, p.N - 1 - n0) * (uint32_t)p.d + piece;
+        // (a scale is loaded by every wavefront that has none of its own to load)
+        sbase = p.xs + (size_t)n0 * p.blocks;
+        soff = (uint32_t)min((wave % NJ) * 64 + lane, p.N - 1 - n0) * (uint32_t)p.blocks * 4;
+    }
+    __device__ __forceinline__ void operator()(int b, int slot) const {
         const uint32_t at = lds0 + slot * S::buffer;
         const int k0 = b * kBlock;
-        if (k0 + kBlock <= p.d) {
+        if (k0 + kBlock <= d) {
 #pragma unroll
             for (int i = 0; i < S::w_loads; ++i) load_lds16(at + (wave * S::w_loads + i) * 1024, woff[i], wbase + k0);
 #pragma unroll
             for (int i = 0; i < S::x_loads; ++i)
                 load_lds16(at + S::w_bytes + (wave * S::x_loads + i) * 1024, xoff[i], xbase + k0);
         } else {  // a last block that is shorter: zeros behind the rows' ends
-            const bool in = k0 + piece < p.d;
-            uintx4 *dst = reinterpret_cast<uintx4 *>(f8_smem + slot * S::buffer) + lane;
+            const bool in = k0 + piece < d;
+            uintx4 *dst = reinterpret_cast<uintx4 *>(smem + slot * S::buffer) + lane;
 #pragma unroll
             for (int i = 0; i < S::w_loads; ++i) {
                 uintx4 v = *reinterpret_cast<const uintx4 *>(wbase + (in ? k0 + woff[i] : 0u));
@@ -151,43 +148,84 @@ __global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p
             }
         }
         load_lds4(at + S::w_bytes + S::x_bytes + (wave % NJ) * 256, soff, sbase + b);
-    };
+    }
+};
+
+// The scales of 128 rows of w (a scalar load: a vector load would be waited for behind the tiles that are in flight)
+typedef const __attribute__((address_space(4))) float *scalar_ptr;
+__device__ __forceinline__ scalar_ptr row_scales(const MatmulF8Params &p, int v0, int wv) {
+    return (scalar_ptr)(uintptr_t)(p.ws + (size_t)min((v0 >> 7) + wv, (p.V - 1) >> 7) * p.blocks);
+}
+
+__device__ __forceinline__ Codes read_codes(const unsigned char *t, int i, int frag) {
+    Codes o;
+    o.piece[0] = *reinterpret_cast<const uintx4 *>(t + i * 16 * kBlock + frag);
+    o.piece[1] = *reinterpret_cast<const uintx4 *>(t + i * 16 * kBlock + (frag ^ 64));
+    return o;
+}
+
+template <typename T, int WV, int NJ>
+__device__ __forceinline__ void store_tile(const MatmulF8Params &p, const floatx4 (&acc)[8][NJ], int v0, int n0) {
+    const bool parts = gridDim.z > 1;
+    const int q = (threadIdx.x & 63) >> 4, c = threadIdx.x & 15;
+    float *part = static_cast<float *>(p.workspace) + (size_t)blockIdx.z * p.N * p.V;
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+        const int n = n0 + j * 16 + c;
+        if (n >= p.N) continue;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int v = v0 + i * 16 + 4 * q;
+            if (v >= p.V) continue;
+            if (parts)
+                store_quad(part, (size_t)n * p.V + v, p.V - v, acc[i][j]);
+            else
+                store_quad(static_cast<T *>(p.out), (size_t)n * p.V + v, p.V - v, acc[i][j]);
+        }
+    }
+}
+
+// T: type of the result.  fp16 results take the codes as they are, fp32 results as halves.
+template <typename T, int WV, int NJ>
+__global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p) {
+    using S = Tile<WV, NJ>;
+    typedef typename std::conditional<sizeof(T) == 4, Halves, Codes>::type Operand;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char f8_smem[];
+    const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wv = wave >> 2, wn = wave & 3;
+    const int v0 = blockIdx.x * S::rows, n0 = blockIdx.y * S::states;
+    const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
+    const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
+    const Loader<WV, NJ> load(p, v0, n0, wave, lane, f8_smem);
 
     floatx4 acc[8][NJ] = {};
     const int frag = c * kBlock + ((q ^ (c & 7)) << 4);
-    // (a scalar load: a vector load would be waited for behind the tiles that are in flight)
-    typedef const __attribute__((address_space(4))) float *scalar_ptr;
-    const scalar_ptr ws = (scalar_ptr)(uintptr_t)(p.ws + (size_t)min((v0 >> 7) + wv, (p.V - 1) >> 7) * p.blocks);
+    const scalar_ptr ws = row_scales(p, v0, wv);
     float sw = ws[b0];
 #pragma unroll
     for (int k = 0; k < S::buffers - 1; ++k)
-        if (b0 + k < b1) load(b0 + k);
+        if (b0 + k < b1) load(b0 + k, k);
     for (int b = b0; b < b1; ++b) {
         if (S::buffers == 3 && b + 1 < b1)
             landed<S::loads>();
         else
             landed<0>();
-        if (b + S::buffers - 1 < b1) load(b + S::buffers - 1);
+        if (b + S::buffers - 1 < b1) load(b + S::buffers - 1, (b - b0 + S::buffers - 1) % S::buffers);
         const float sw_next = ws[min(b + 1, b1 - 1)];
         const unsigned char *buf = f8_smem + ((b - b0) % S::buffers) * S::buffer;
         const unsigned char *wt = buf + wv * 128 * kBlock, *xt = buf + S::w_bytes + wn * NJ * 16 * kBlock;
         const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * NJ * 16 + c;
-        auto operand = [&](const unsigned char *t, int i) {
-            Codes o;
-            o.piece[0] = *reinterpret_cast<const uintx4 *>(t + i * 16 * kBlock + frag);
-            o.piece[1] = *reinterpret_cast<const uintx4 *>(t + i * 16 * kBlock + (frag ^ 64));
-            return Operand(o);
-        };
         float s[NJ];
         Operand x[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
-            x[j] = operand(xt, j);
+            x[j] = Operand(read_codes(xt, j, frag));
             s[j] = st[j * 16] * sw;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const Operand w = operand(wt, i);
+            const Operand w(read_codes(wt, i, frag));
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 const floatx4 t = block_product(w, x[j]);
@@ -197,22 +235,84 @@ __global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p
         }
         sw = sw_next;
     }
-    const bool parts = gridDim.z > 1;
-    float *part = static_cast<float *>(p.workspace) + (size_t)blockIdx.z * p.N * p.V;
+    store_tile<T, WV, NJ>(p, acc, v0 + wv * 128, n0 + wn * NJ * 16);
+}
+
+__device__ __forceinline__ void meet() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+__device__ __forceinline__ void all_landed() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+
+// The same with eight wavefronts, two on a SIMD, of which one reads a block's operands from LDS into registers while the
+// other multiplies: wavefronts 4..7 are half a block behind 0..3.  Phase 2b: 0..3 read block b, 4..7 multiply block b - 1;
+// phase 2b + 1: 0..3 multiply block b, 4..7 read it.  A phase begins with a meeting of all; behind the one of phase 2b, when
+// block b - 1 has been read by all, all ask for block b + 1 in its place, and wait for it before the meeting of phase 2b + 2.
+template <typename T, int NJ>
+__global__ __launch_bounds__(512, 2) void matmul_f8_turns_kernel(MatmulF8Params p) {
+    using S = Tile<2, NJ>;
+    typedef typename std::conditional<sizeof(T) == 4, Halves, Codes>::type Operand;
+    extern __shared__ __attribute__((aligned(1024))) unsigned char f8_smem[];
+    const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wv = wave >> 2, wn = wave & 3;
+    const int v0 = blockIdx.x * S::rows, n0 = blockIdx.y * S::states;
+    const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
+    const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
+    const Loader<2, NJ> load(p, v0, n0, wave, lane, f8_smem);
+
+    floatx4 acc[8][NJ] = {};
+    const int frag = c * kBlock + ((q ^ (c & 7)) << 4);
+    const scalar_ptr ws = row_scales(p, v0, wv);
+    load(b0, 0);
+    all_landed();
+    if (wv == 1) {
+        meet();
+        if (b0 + 1 < b1) load(b0 + 1, 1);
+    }
+    int slot = 0;
+    for (int b = b0; b < b1; ++b, slot ^= 1) {
+        meet();
+        if (wv == 0 && b + 1 < b1) load(b + 1, slot ^ 1);
+        const float sw = ws[b];
+        const unsigned char *buf = f8_smem + slot * S::buffer;
+        const unsigned char *wt = buf + wv * 128 * kBlock, *xt = buf + S::w_bytes + wn * NJ * 16 * kBlock;
+        const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * NJ * 16 + c;
+        Codes xc[NJ], wc[8];
+        float s[NJ];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        const int n = n0 + (wn * NJ + j) * 16 + c;
-        if (n >= p.N) continue;
+        for (int j = 0; j < NJ; ++j) {
+            xc[j] = read_codes(xt, j, frag);
+            s[j] = st[j * 16];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wc[i] = read_codes(wt, i, frag);
+        if (wv == 1) all_landed();
+        meet();
+        if (wv == 1 && b + 2 < b1) load(b + 2, slot);
+        Operand x[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+            x[j] = Operand(xc[j]);
+            s[j] *= sw;
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int v = v0 + wv * 128 + i * 16 + 4 * q;
-            if (v >= p.V) continue;
-            if (parts)
-                store_quad(part, (size_t)n * p.V + v, p.V - v, acc[i][j]);
-            else
-                store_quad(static_cast<T *>(p.out), (size_t)n * p.V + v, p.V - v, acc[i][j]);
+            const Operand w(wc[i]);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                const floatx4 t = block_product(w, x[j]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[j], t[e], acc[i][j][e]);
+            }
         }
+        if (wv == 0) all_landed();
     }
+    if (wv == 0) meet();
+    store_tile<T, 2, NJ>(p, acc, v0 + wv * 128, n0 + wn * NJ * 16);
 }
 
 // Sums of the parts, in their order
@@ -261,6 +361,17 @@ hipError_t launch_tile(const MatmulF8Params &p, int parts, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <typename T, int NJ>
+hipError_t launch_turns(const MatmulF8Params &p, int parts, hipStream_t s) {
+    using S = Tile<2, NJ>;
+    const auto kern = matmul_f8_turns_kernel<T, NJ>;
+    const int lds = 2 * S::buffer;
+    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    const dim3 grid((p.V + S::rows - 1) / S::rows, (p.N + S::states - 1) / S::states, parts);
+    hipLaunchKernelGGL(kern, grid, dim3(S::threads), lds, s, p);
+    return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s) {
     hipError_t e;
@@ -270,8 +381,11 @@ hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s)
         case 13: e = launch_tile<T, 1, 3>(p, sh.parts, s); break;
         case 14: e = launch_tile<T, 1, 4>(p, sh.parts, s); break;
         case 22: e = launch_tile<T, 2, 2>(p, sh.parts, s); break;
+        case 32: e = launch_turns<T, 2>(p, sh.parts, s); break;
         case 23: e = launch_tile<T, 2, 3>(p, sh.parts, s); break;
+        case 33: e = launch_turns<T, 3>(p, sh.parts, s); break;
         case 24: e = launch_tile<T, 2, 4>(p, sh.parts, s); break;
+        case 34: e = launch_turns<T, 4>(p, sh.parts, s); break;
         default: return hipErrorInvalidValue;
     }
     if (e != hipSuccess || sh.parts == 1) return e;
