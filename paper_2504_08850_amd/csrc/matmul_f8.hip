@@ -327,12 +327,124 @@ __global__ __launch_bounds__(256) void matmul_f8_join_kernel(const float *part, 
     store_quad(out, i, left, sum);
 }
 
+// ---- few states -------------------------------------------------------------------------------------------------------
+// Up to 16 rows of x: a stream over w.  The elements are cut over the wavefronts of a workgroup, CPW blocks each, whose x
+// stays in registers as codes; a tile is 16 rows of w, a unit one to four of them, and a wavefront has kAhead blocks of 16 rows
+// (2 KB each) in flight at any time, across tiles and units.  Loads take whole 128-byte lines of eight rows with the
+// non-temporal hint; two of them become an operand by exchanging halves of 16 lanes.  The wavefronts' sums meet in LDS once
+// per unit and are added in ascending order of elements.
+constexpr int kAhead = 4;
+constexpr int kStreamBlocks = 64;  // of a pass: 16 wavefronts of 4
+
+template <typename T, int CPW, bool WHOLE>
+__global__ __launch_bounds__(1024) void matmul_f8_stream_kernel(MatmulF8Params p, int unit_tiles) {
+    constexpr int RING = kAhead / CPW;  // tiles in flight
+    typedef typename std::conditional<sizeof(T) == 4, Halves, Codes>::type Operand;
+    extern __shared__ __attribute__((aligned(16))) floatx4 f8_sums[];  // [tile][wavefront][lane]
+    const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+    const int part0 = (int)((long long)p.blocks * blockIdx.y / gridDim.y);
+    const int part1 = (int)((long long)p.blocks * (blockIdx.y + 1) / gridDim.y);
+    const int first = part0 + wave * CPW;
+    const int units = (p.V + 16 * unit_tiles - 1) / (16 * unit_tiles);
+
+    // a lane's piece of a load: piece q + 4 * (c / 8) of row c % 8 (and 8 + c % 8)
+    const int piece = (q + 4 * (c >> 3)) * 16, sub = c & 7;
+    uintx4 ring[RING][CPW][2];
+    // tile t of a unit, or of the one behind it
+    auto load = [&](int unit, int next, int t, int k, uintx4 (&r)[2]) {
+        const int row = (t < unit_tiles ? unit * unit_tiles + t : next * unit_tiles + t - unit_tiles) * 16, last = p.V - 1 - row;
+        const uint8_t *base = p.w + (last < 0 ? (long long)p.V - 1 : (long long)row) * p.d + (size_t)first * kBlock;
+        const bool have = WHOLE || (first + k < part1 && (first + k) * kBlock + piece < p.d);
+        const int col = have ? k * kBlock + piece : -first * kBlock;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int off = max(min(sub + 8 * h, last), 0) * p.d + col;
+            const uint8_t *at = WHOLE ? base + (uint32_t)off : base + off;
+            r[h] = __builtin_nontemporal_load(reinterpret_cast<const uintx4 *>(at));
+        }
+    };
+    int unit = blockIdx.x;
+#pragma unroll
+    for (int u = 0; u < RING; ++u)
+#pragma unroll
+        for (int k = 0; k < CPW; ++k) load(unit, unit, u, k, ring[u][k]);
+
+    Codes x[CPW];
+    float sx[CPW];
+    bool in[CPW][2];  // whether a lane's pieces exist
+#pragma unroll
+    for (int k = 0; k < CPW; ++k) {
+        const int b = first + k;
+        const uint8_t *row = p.x + (size_t)min(c, p.N - 1) * p.d;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int at = b * kBlock + (q + 4 * h) * 16;
+            in[k][h] = WHOLE || (b < part1 && at < p.d);
+            uintx4 v = *reinterpret_cast<const uintx4 *>(row + (in[k][h] ? at : 0));
+            if (!in[k][h]) v = uintx4{0, 0, 0, 0};
+            x[k].piece[h] = v;
+        }
+        sx[k] = WHOLE || b < part1 ? p.xs[(size_t)min(c, p.N - 1) * p.blocks + min(b, part1 - 1)] : 0.f;
+    }
+
+    for (; unit < units; unit += gridDim.x) {
+        const int next = min(unit + (int)gridDim.x, units - 1);
+        const scalar_ptr ws = row_scales(p, unit * 16 * unit_tiles, 0);
+        float f[CPW];
+#pragma unroll
+        for (int k = 0; k < CPW; ++k) f[k] = sx[k] * ws[min(first + k, p.blocks - 1)];
+#pragma unroll 1
+        for (int t0 = 0; t0 < unit_tiles; t0 += RING) {
+#pragma unroll
+            for (int u = 0; u < RING; ++u) {
+                floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < CPW; ++k) {
+                    Codes w;
+                    w.piece[0] = ring[u][k][0];
+                    w.piece[1] = ring[u][k][1];
+                    whole_lines(w.piece[0], w.piece[1]);
+                    load(unit, next, t0 + u + RING, k, ring[u][k]);
+                    if (!WHOLE) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+                            if (!in[k][h]) w.piece[h] = uintx4{0, 0, 0, 0};
+                    }
+                    Codes xk = x[k];
+                    if (sizeof(T) == 4)  // the halves of x are formed again for every tile: kept, they would cost a workgroup per CU
+                        asm volatile("" : "+v"(xk.all));
+                    const floatx4 s = block_product(Operand(w), Operand(xk));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[e] = fmaf(f[k], s[e], acc[e]);
+                }
+                f8_sums[((t0 + u) * waves + wave) * kWave + lane] = acc;
+            }
+        }
+        __syncthreads();
+        for (int t = wave; t < unit_tiles; t += waves) {
+            floatx4 sum = f8_sums[t * waves * kWave + lane];
+            for (int w = 1; w < waves; ++w) sum += f8_sums[(t * waves + w) * kWave + lane];
+            const int v = (unit * unit_tiles + t) * 16 + 4 * q;
+            if (c < p.N && v < p.V) {
+                if (gridDim.y > 1)
+                    store_quad(static_cast<float *>(p.workspace) + (size_t)blockIdx.y * p.N * p.V, (size_t)c * p.V + v,
+                               p.V - v, sum);
+                else
+                    store_quad(static_cast<T *>(p.out), (size_t)c * p.V + v, p.V - v, sum);
+            }
+        }
+        __syncthreads();
+    }
+}
+
 struct Shape {
     int wv, nj, parts;
 };
 
 Shape shape_of(int N, int V, int d) {
     const int blocks = (d + kBlock - 1) / kBlock;
+    if (N <= 16) return Shape{0, 0, (blocks + kStreamBlocks - 1) / kStreamBlocks};
     Shape best{1, (N + 63) / 64 > 4 ? 4 : (N + 63) / 64, 1};
     if (N > 256) {
         long cost = LONG_MAX;
@@ -348,6 +460,35 @@ Shape shape_of(int N, int V, int d) {
     const long tiles = (long)((V + 128 * best.wv - 1) / (128 * best.wv)) * ((N + 64 * best.nj - 1) / (64 * best.nj));
     while (best.parts < 8 && tiles * best.parts * 2 <= 256 && blocks >= best.parts * 2 * 4) best.parts *= 2;
     return best;
+}
+
+template <typename T, int CPW, bool WHOLE>
+hipError_t launch_stream(const MatmulF8Params &p, int parts, hipStream_t s) {
+    const int blocks = (p.blocks + parts - 1) / parts, waves = (blocks + CPW - 1) / CPW;
+    const auto kern = matmul_f8_stream_kernel<T, CPW, WHOLE>;
+    // two workgroups of up to eight wavefronts fit on a CU; smaller units where larger ones would leave CUs without any
+    // (1024 x 5120 by one state: 13.7 us in units of four, 6.9 of one)
+    const int most = 256 * (waves > 8 ? 1 : 2), tiles = (p.V + 15) / 16;
+    int unit = 4;
+    while (unit > kAhead / CPW && (tiles + unit - 1) / unit * parts < most * 3 / 4) unit /= 2;
+    const int units = (tiles + unit - 1) / unit, lds = unit * waves * kWave * (int)sizeof(floatx4);  // at most 64 KB
+    hipLaunchKernelGGL(kern, dim3(units < most ? units : most, parts), dim3(waves * kWave), lds, s, p, unit);
+    return hipGetLastError();
+}
+
+template <typename T>
+hipError_t launch_few(const MatmulF8Params &p, int parts, hipStream_t s) {
+    const int blocks = (p.blocks + parts - 1) / parts;
+    const int cpw = blocks <= 8 ? 1 : blocks <= 16 ? 2 : 4;
+    const bool whole = p.d % (kBlock * cpw * parts) == 0;
+    switch (cpw * 2 + whole) {
+        case 2: return launch_stream<T, 1, false>(p, parts, s);
+        case 3: return launch_stream<T, 1, true>(p, parts, s);
+        case 4: return launch_stream<T, 2, false>(p, parts, s);
+        case 5: return launch_stream<T, 2, true>(p, parts, s);
+        case 8: return launch_stream<T, 4, false>(p, parts, s);
+        default: return launch_stream<T, 4, true>(p, parts, s);
+    }
 }
 
 template <typename T, int WV, int NJ>
@@ -376,6 +517,7 @@ template <typename T>
 hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s) {
     hipError_t e;
     switch (sh.wv * 10 + sh.nj) {
+        case 0: e = launch_few<T>(p, sh.parts, s); break;
         case 11: e = launch_tile<T, 1, 1>(p, sh.parts, s); break;
         case 12: e = launch_tile<T, 1, 2>(p, sh.parts, s); break;
         case 13: e = launch_tile<T, 1, 3>(p, sh.parts, s); break;
