@@ -7,7 +7,7 @@
 // Forward: one pass over the logits.  A lane keeps a reference r (an element of its own, at most 8 below its maximum), the
 // sums of exp(x - r) and exp(x - r)(x - r), and its largest element; 16 bytes are loaded per lane and step, rows may start at
 // any element (what lies before the first and behind the last whole 16 bytes is done one element per lane).  A logit of -inf
-// adds nothing (its difference is cut at -200, whose exponential is 0 in fp32); NaN and +inf make the sum NaN, which is
+// adds nothing (its t is cut at -300, and 2^-300 is 0 in fp32); NaN and +inf make the sum NaN, which is
 // looked at once at the end.
 // Alternatives cost the pass only the lanes' maxima.  At its end the lanes are folded to 64 groups, whose n-th largest
 // maximum tau is at most the n-th largest logit: only the few lanes that hold something of at least tau read their own
@@ -29,8 +29,9 @@ constexpr int kT = 512;  // threads of a workgroup
 constexpr int kWaves = kT / kWave;
 constexpr int kUnroll = 4;
 constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kSlack = 8.f;   // how far a lane's reference may lie below its maximum
-constexpr float kFloor = -200.f;
+constexpr float kFloor = -300.f;
 constexpr int kMaxParts = 16;  // of a row
 
 template <typename E>
@@ -44,6 +45,10 @@ __device__ __forceinline__ Granule<E> load_granule(const E *p) {
     Granule<E> g;
     *reinterpret_cast<uintx4 *>(&g) = *reinterpret_cast<const uintx4 *>(p);
     return g;
+}
+template <typename E>
+__device__ __forceinline__ Granule<E> load_granule_once(const E *p) {
+    return __builtin_bit_cast(Granule<E>, __builtin_nontemporal_load(reinterpret_cast<const uintx4 *>(p)));
 }
 
 // A row: `head` elements, then `whole` granules at 16-byte boundaries, then the rest
@@ -60,52 +65,58 @@ struct RowView {
     __device__ int index(int g) const { return head + g * Granule<E>::n; }
 };
 
+// Sums about a reference r, in base 2: t = (x - r) log2 e.  fp16 logits form t in one mixed instruction from x and the rounded
+// product r log2 e (RowStats puts back what was rounded off); fp32 logits, which may be near the ends of their type, from x - r.
+template <typename E>
 struct LaneSum {
-    float r, s, sx;  // reference, sum of exp(x - r), sum of exp(x - r)(x - r)
-    float best;
-    int at;  // granule of best
+    static constexpr bool kMixed = sizeof(E) == 2;
+    static constexpr float kLowest = kMixed ? -1e6f : -FLT_MAX;
+    float r;      // an element, or kLowest while there is none
+    float r2;     // kMixed: r log2 e
+    float s, st;  // sum of 2^t, of 2^t t
+
+    __device__ __forceinline__ void about(float ref) {
+#pragma clang fp contract(off)  // the rounded product, also where it is subtracted
+        r = ref;
+        r2 = kMixed ? ref * kLog2e : 0.f;
+    }
+    __device__ __forceinline__ explicit LaneSum(float ref) : s(0.f), st(0.f) { about(ref); }
+    __device__ __forceinline__ float distance(float x) const { return kMixed ? fmaf(x, kLog2e, -r2) : (x - r) * kLog2e; }
+    __device__ __forceinline__ void add(float x) {
+        const float t = distance(x), e = __builtin_amdgcn_exp2f(t);
+        s += e;
+        st = fmaf(e, fmaxf(t, kFloor), st);
+    }
+    // The same sums about M >= r
+    __device__ __forceinline__ void move(float M) {
+        const LaneSum to(M);
+        if (s == 0.f) {  // empty: r may be anything
+            st = 0.f;
+        } else {
+            const float d = kMixed ? r2 - to.r2 : (r - M) * kLog2e, f = __builtin_amdgcn_exp2f(d);
+            st = f > 0.f ? (st + s * d) * f : 0.f;
+            s *= f;
+        }
+        r = to.r;
+        r2 = to.r2;
+    }
+    // ... about the largest of the elements to come
+    __device__ __forceinline__ void raise(float c) {
+        if (c > r + kSlack) {
+            if (s > 0.f)
+                move(c);
+            else
+                about(c);  // (nothing yet; or NaN, which stays)
+        }
+    }
 };
 
-__device__ __forceinline__ void raise(LaneSum &a, float c) {
-    if (c > a.r + kSlack) {
-        if (a.s > 0.f) {
-            const float d = a.r - c, f = exp2f(d * kLog2e);
-            a.sx = f > 0.f ? (a.sx + a.s * d) * f : 0.f;
-            a.s *= f;
-        }
-        a.r = c;
-    }
-}
-
-__device__ __forceinline__ void add(LaneSum &a, float x) {
-    const float t = x - a.r, e = __builtin_amdgcn_exp2f(t * kLog2e);
-    a.s += e;
-    a.sx = fmaf(e, fmaxf(t, kFloor), a.sx);
-}
-
 template <typename E>
-__device__ __forceinline__ void take(LaneSum &a, const Granule<E> &g, int at) {
-    float c = (float)g.v[0];
+__device__ __forceinline__ float largest(const Granule<E> &g) {
+    float c = -INFINITY;
 #pragma unroll
-    for (int j = 1; j < Granule<E>::n; ++j) c = fmaxf(c, (float)g.v[j]);
-    raise(a, c);
-#pragma unroll
-    for (int j = 0; j < Granule<E>::n; ++j) add(a, (float)g.v[j]);
-    if (c > a.best) {
-        a.best = c;
-        a.at = at;
-    }
-}
-
-// Joins sums (r, s, sx) of which each may be empty (s == 0) into one about M >= every r
-__device__ __forceinline__ void shift(float r, float &s, float &sx, float M) {
-    if (s == 0.f) {
-        sx = 0.f;
-        return;
-    }
-    const float d = fmaxf(r - M, kFloor), f = exp2f(d * kLog2e);
-    sx = (sx + s * d) * f;
-    s *= f;
+    for (int j = 0; j < Granule<E>::n; ++j) c = fmaxf(c, (float)g.v[j]);
+    return c;
 }
 
 __device__ __forceinline__ float wave_max(float v) {
@@ -121,12 +132,13 @@ __device__ __forceinline__ float wave_max(float v) {
 struct RowStats {
     float m, log_sum, entropy;
     bool bad, empty;
-    __device__ RowStats(float M, float s, float sx) {
+    // sums about M, in base 2; mixed: about the rounded M log2 e
+    __device__ RowStats(float M, float s, float st, bool mixed) {
         bad = !(s == s);
         empty = s == 0.f;
-        const float nan = quiet_nan();
-        log_sum = bad ? nan : empty ? -INFINITY : logf(s);
-        entropy = bad ? nan : empty ? 0.f : fmaxf(log_sum - sx / s, 0.f);
+        const float nan = quiet_nan(), ln = logf(s), off = mixed ? fmaf(-M, kLog2e, M * kLog2e) : 0.f;
+        log_sum = bad ? nan : empty ? -INFINITY : fmaf(off, kLn2, ln);
+        entropy = bad ? nan : empty ? 0.f : fmaxf(ln - kLn2 * (st / s), 0.f);
         m = bad ? nan : M;
     }
     __device__ float log_prob(float x) const { return bad ? quiet_nan() : empty ? -INFINITY : (x - m) - log_sum; }
@@ -152,29 +164,54 @@ __device__ __forceinline__ void write_alternative(const LogprobsParams &p, int n
     p.top_logprobs[(size_t)n * p.K + k] = st.bad ? quiet_nan() : none ? -INFINITY : st.log_prob(x);
 }
 
+__device__ __forceinline__ int from_lane_below(int v) {
+    constexpr int kDppWaveShr1 = 0x138;
+    return __builtin_amdgcn_update_dpp(v, v, kDppWaveShr1, 0xF, 0xF, false);
+}
+
+// The K-th largest of the groups' maxima, or a little less: floats as integers of the same order, whose last six bits are the
+// group, so that no two are equal.  Each wavefront counts for GROUPS / WAVES of them; tau is there behind the next meeting.
+__device__ __forceinline__ uint32_t ordered(float v) {
+    const uint32_t bits = __builtin_bit_cast(uint32_t, v);
+    return bits ^ (bits >> 31 ? 0xffffffffu : 0x80000000u);
+}
+template <int GROUPS, int WAVES>
+__device__ __forceinline__ void kth_largest(float c, int K, float *tau) {
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const uint32_t key = (lane < GROUPS ? ordered(c) & ~63u : 0u) | (63 - lane);
+#pragma unroll
+    for (int k = 0; k < GROUPS / WAVES; ++k) {
+        const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)key, wave * (GROUPS / WAVES) + k);
+        if (__popcll(__ballot(key > mine)) == K - 1 && lane == 0) {
+            const uint32_t b = mine & ~63u;
+            const float t = __builtin_bit_cast(float, b >> 31 ? b ^ 0x80000000u : ~b);
+            *tau = t == t ? t : -INFINITY;  // (below -inf, in this order, there are NaNs)
+        }
+    }
+}
+
 // A wavefront's list, entry i on lane i, by logit and then by id
 struct TopList {
     float v;
     int id;
     float last;  // the K-th
-    __device__ TopList() : v(-INFINITY), id(INT_MAX), last(-INFINITY) {}
-    // x, i: the same on all lanes; ids come in ascending order
+    int last_id;
+    __device__ TopList() : v(-INFINITY), id(INT_MAX), last(-INFINITY), last_id(INT_MAX) {}
+    // x, i: the same on all lanes
     __device__ __forceinline__ void insert(float x, int i, int K) {
         const int lane = threadIdx.x & (kWave - 1);
-        const int pos = __popcll(__ballot(v >= x));
-        const float uv = __shfl_up(v, 1, kWave);
-        const int ui = __shfl_up(id, 1, kWave);
+        const int pos = __popcll(__ballot(v > x || (v == x && id < i)));
+        const float uv = __builtin_bit_cast(float, from_lane_below(__builtin_bit_cast(int, v)));
+        const int ui = from_lane_below(id);
         v = lane < pos ? v : lane == pos ? x : uv;
         id = lane < pos ? id : lane == pos ? i : ui;
         last = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), K - 1));
+        last_id = __builtin_amdgcn_readlane(id, K - 1);
     }
-    // lanes hold n values each (first id `at`), in ascending order of ids over the lanes; has: the lane holds any
+    // n values on each lane that has any, the first with id `at`; c: the largest of them
     template <int n, typename E>
-    __device__ __forceinline__ void scan(const E *x, int at, bool has, float tau, int K) {
-        float c = -INFINITY;
-#pragma unroll
-        for (int j = 0; j < n; ++j) c = fmaxf(c, (float)x[j]);
-        unsigned long long who = __ballot(has && c >= tau && c > last);
+    __device__ __forceinline__ void scan(const E *x, float c, int at, bool has, float tau, int K) {
+        unsigned long long who = __ballot(has && c >= tau && c >= last && c > -INFINITY);
         while (who) {
             const int l = __ffsll(who) - 1;
             who &= who - 1;
@@ -183,209 +220,286 @@ struct TopList {
             for (int j = 0; j < n; ++j) {
                 const float v1 = __builtin_bit_cast(
                     float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, (float)x[j]), l));
-                if (v1 >= tau && v1 > last) insert(v1, first + j, K);
+                if (v1 >= tau && (v1 > last || (v1 == last && first + j < last_id))) insert(v1, first + j, K);
             }
         }
     }
 };
 
-template <typename E>
-__global__ __launch_bounds__(kT) void logprobs_kernel(LogprobsParams p) {
-    constexpr int G = Granule<E>::n;
+// Calls put(rank, x, id) on one lane for each of the C entries (in LDS) whose rank is below K, by x and then by id
+template <int WAVES, typename F>
+__device__ __forceinline__ void rank_entries(const float *v, const int *id, int C, int K, const F &put) {
+    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const float mv = lane < C ? v[lane] : -INFINITY;
+    const int mi = lane < C ? id[lane] : INT_MAX;
+    for (int e = wave; e < C; e += WAVES) {
+        const float x = v[e];
+        const int i = id[e];
+        int rank = __popcll(__ballot(mv > x || (mv == x && mi < i)));
+        for (int o = kWave; o < C; o += kWave) {
+            const bool has = o + lane < C;
+            const float ov = has ? v[o + lane] : -INFINITY;
+            const int oi = has ? id[o + lane] : INT_MAX;
+            rank += __popcll(__ballot(ov > x || (ov == x && oi < i)));
+        }
+        if (rank < K && lane == 0) put(rank, x, i);
+    }
+}
+
+// What a workgroup's wavefronts leave for its end: their sums, and the entries of their lists in any order
+template <int WAVES>
+struct RowEnd {
+    float s[WAVES], st[WAVES];
+    int entries;
+    float v[WAVES * SPECEE_TOP_MAX];
+    int id[WAVES * SPECEE_TOP_MAX];
+
+    // Behind a meeting of the workgroup that follows entries = 0
+    __device__ __forceinline__ void leave(float sum, float sumt, const TopList &top, int K) {
+        const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+        sum = wave_sum(sum);
+        sumt = wave_sum(sumt);
+        if (lane == 0) {
+            s[wave] = sum;
+            st[wave] = sumt;
+        }
+        const bool mine = lane < K && top.v > -INFINITY;
+        const int c = __popcll(__ballot(mine));
+        int first = 0;
+        if (lane == 0 && c) first = atomicAdd(&entries, c);
+        first = __builtin_amdgcn_readfirstlane(first);
+        if (mine) {
+            v[first + lane] = top.v;
+            id[first + lane] = top.id;
+        }
+    }
+    // Behind another: the row's or the part's outputs.  An entry's place is its rank: every lane holds one (or more), every
+    // wavefront ranks its share of them.
+    template <typename E>
+    __device__ __forceinline__ void write(const LogprobsParams &p, int n, int part, const E *row, float M) const {
+        const int tid = threadIdx.x;
+        float S = 0.f, ST = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            S += s[w];
+            ST += st[w];
+        }
+        const RowStats stats(M, S, ST, LaneSum<E>::kMixed);
+        const size_t at = (size_t)n * p.parts + part;
+        if (p.parts > 1) {
+            if (tid == 0) {
+                p.part_sums[at * 4] = M;
+                p.part_sums[at * 4 + 1] = S;
+                p.part_sums[at * 4 + 2] = ST;
+            }
+        } else {
+            if (tid == 0) write_row(p, n, stats);
+            write_tokens(p, n, row, stats, tid);
+        }
+        if (p.K == 0) return;
+        const int C = entries;
+        auto put = [&](int k, float x, int i) {
+            if (p.parts > 1) {
+                p.part_vals[at * p.K + k] = x;
+                p.part_ids[at * p.K + k] = i;
+            } else {
+                write_alternative(p, n, k, stats, x, i);
+            }
+        };
+        rank_entries<WAVES>(v, id, C, p.K, put);
+        if (tid >= C && tid < p.K) put(tid, -INFINITY, INT_MAX);
+    }
+};
+
+__device__ __forceinline__ float row16_max(float v) {
+    v = fmaxf(v, dpp_f32<kDppXor1>(v));
+    v = fmaxf(v, dpp_f32<kDppXor2>(v));
+    v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+    return fmaxf(v, dpp_f32<kDppMirror>(v));
+}
+
+// A row (or part) that a workgroup holds in registers, U granules per lane: the maximum first, then the sums about it and the
+// alternatives, all from the registers.
+template <typename E, int T, int U>
+__global__ __launch_bounds__(T, 8) void logprobs_held_kernel(LogprobsParams p) {
+    constexpr int G = Granule<E>::n, WAVES = T / kWave, GROUPS = T / 16;
     const int n = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
     const int g0 = (int)((long long)row.whole * part / p.parts), g1 = (int)((long long)row.whole * (part + 1) / p.parts);
     const int heads = part == 0 ? row.head : 0, tails = part == p.parts - 1 ? row.tail : 0;
     const E *body = row.p + row.head, *end = row.p + p.V - row.tail;
+    __shared__ float groups[GROUPS], tau;
+    __shared__ RowEnd<WAVES> last;
 
-    LaneSum a{-FLT_MAX, 0.f, 0.f, -INFINITY, 0};
-    int g = g0 + tid;
-    for (; g + (kUnroll - 1) * kT < g1; g += kUnroll * kT) {
-        Granule<E> x[kUnroll];
+    uintx4 raw[U];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule(body + (size_t)(g + u * kT) * G);
+    for (int u = 0; u < U; ++u) raw[u] = uintx4{0, 0, 0, 0};
+    if (g0 < g1) {
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) take(a, x[u], g + u * kT);
-    }
-    for (; g < g1; g += kT) take(a, load_granule(body + (size_t)g * G), g);
-    if (tid < heads + tails) {
-        const float x = (float)(tid < heads ? row.p[tid] : end[tid - heads]);
-        raise(a, x);
-        add(a, x);
-    }
-
-    // the workgroup's maximum and sums about it
-    __shared__ float red[3][kWaves];
-    __shared__ float lane_best[kT];
-    {
-        float m = a.best;
-        if (tid < heads + tails) m = fmaxf(m, (float)(tid < heads ? row.p[tid] : end[tid - heads]));
-        m = wave_max(m);
-        if (lane == 0) red[0][wave] = m;
-    }
-    lane_best[tid] = a.best;
-    __syncthreads();
-    float M = red[0][0];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, red[0][w]);
-    shift(a.r, a.s, a.sx, M);
-    const float ws = wave_sum(a.s), wx = wave_sum(a.sx);
-    if (lane == 0) {
-        red[1][wave] = ws;
-        red[2][wave] = wx;
-    }
-    __syncthreads();
-    float s = 0.f, sx = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        s += red[1][w];
-        sx += red[2][w];
-    }
-    const RowStats st(M, s, sx);
-    float *sums = p.part_sums + ((size_t)n * p.parts + part) * 4;
-    if (p.parts > 1) {
-        if (tid == 0) {
-            sums[0] = M;
-            sums[1] = s;
-            sums[2] = sx;
+        for (int u = 0; u < U; ++u) {
+            const int g = min(g0 + u * T + tid, g1 - 1);
+            raw[u] = __builtin_nontemporal_load(reinterpret_cast<const uintx4 *>(body + (size_t)g * G));
         }
-    } else {
-        if (tid == 0) write_row(p, n, st);
-        write_tokens(p, n, row.p, st, tid);
     }
-    if (p.K == 0) return;
-
-    // tau: the K-th largest of 64 groups of lanes
-    float tau;
-    {
-        float c = lane_best[lane];
+    float xe = -INFINITY;  // one of the elements before and behind the granules
+    if (tid < heads + tails) xe = (float)(tid < heads ? row.p[tid] : end[tid - heads]);
+    if (tid == 0) last.entries = 0;
+    float c = xe == xe ? xe : -INFINITY;
+    const uint32_t nothing = sizeof(E) == 4 ? 0xff800000u : 0xfc00fc00u;  // -inf
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) c = fmaxf(c, lane_best[w * kWave + lane]);
-        int rank = 0;
-#pragma unroll 8
-        for (int l = 0; l < kWave; ++l) {
-            const float o = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), l));
-            rank += o > c || (o == c && l < lane);
-        }
-        const int l = __ffsll(__ballot(rank == p.K - 1)) - 1;
-        tau = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), l));
+    for (int u = 0; u < U; ++u) {
+        if (g0 + u * T + tid >= g1) raw[u] = uintx4{nothing, nothing, nothing, nothing};
+        c = fmaxf(c, largest(__builtin_bit_cast(Granule<E>, raw[u])));
+        // (fp16 logits are widened again below: kept as floats they would cost half of the workgroups that a CU holds)
+        if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
     }
-    // the lanes that read again, in ascending order
-    __shared__ int sel[kT], count[kWaves + 1];
-    const bool again = a.best >= tau && a.best > -INFINITY;
-    const unsigned long long mask = __ballot(again);
-    if (lane == 0) count[wave] = __popcll(mask);
-    __shared__ int entries;
-    if (tid == 0) entries = 0;
+    c = row16_max(c);
+    if ((lane & 15) == 0) groups[tid / 16] = c;
     __syncthreads();
-    int before = 0, nsel = 0;
+    c = lane < GROUPS ? groups[lane] : -INFINITY;
+    if (p.K) kth_largest<GROUPS, WAVES>(c, p.K, &tau);
+    const float M = wave_max(c);
+    LaneSum<E> a(fmaxf(M, LaneSum<E>::kLowest));
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        before += w < wave ? count[w] : 0;
-        nsel += count[w];
+    for (int u = 0; u < U; ++u) {
+        const Granule<E> x = __builtin_bit_cast(Granule<E>, raw[u]);
+#pragma unroll
+        for (int j = 0; j < G; ++j) a.add((float)x.v[j]);
+        if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
     }
-    if (again) sel[before + __popcll(mask & ((1ull << lane) - 1))] = tid;
-    __syncthreads();
-
+    a.add(xe);
     TopList top;
-    if (wave == 0 && heads) top.scan<1>(row.p + (lane < heads ? lane : 0), lane, lane < heads, tau, p.K);
-    const int steps = (g1 - g0 + kT - 1) / kT, todo = steps * nsel;
-    for (int e0 = wave * kWave; e0 < todo; e0 += kUnroll * kT) {
-        Granule<E> x[kUnroll];
-        int at[kUnroll];
+    if (p.K) {
+        __syncthreads();
+        const float least = tau;
+        if (wave == 0 && heads) top.scan<1>(&xe, xe, lane, lane < heads, least, p.K);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int e = e0 + u * kT + lane, i = e / nsel;
-            const int gi = g0 + i * kT + sel[e < todo ? e - i * nsel : 0];
-            at[u] = e < todo && gi < g1 ? gi : -1;
-            x[u] = load_granule(body + (size_t)(at[u] >= 0 ? at[u] : g0) * G);
+        for (int u = 0; u < U; ++u) {
+            const int g = g0 + u * T + tid;
+            const Granule<E> x = __builtin_bit_cast(Granule<E>, raw[u]);
+            top.scan<G>(x.v, largest(x), row.index(g), g < g1, least, p.K);
         }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) top.scan<G>(x[u].v, row.index(at[u]), at[u] >= 0, tau, p.K);
+        if (wave == 0 && tails)
+            top.scan<1>(&xe, xe, p.V - row.tail + lane - heads, lane >= heads && lane < heads + tails, least, p.K);
     }
-    if (wave == 0 && tails) top.scan<1>(end + (lane < tails ? lane : 0), p.V - row.tail + lane, lane < tails, tau, p.K);
-
-    // the lists' entries, in any order, each to the place that its rank gives it
-    __shared__ float ev[kWaves * SPECEE_TOP_MAX];
-    __shared__ int ei[kWaves * SPECEE_TOP_MAX];
-    {
-        const bool mine = lane < p.K && top.v > -INFINITY;
-        const int c = __popcll(__ballot(mine));
-        int first = 0;
-        if (lane == 0 && c) first = atomicAdd(&entries, c);
-        first = __builtin_amdgcn_readfirstlane(first);
-        if (mine) {
-            ev[first + lane] = top.v;
-            ei[first + lane] = top.id;
-        }
-    }
+    last.leave(a.s, a.st, top, p.K);
     __syncthreads();
-    const int C = entries;
-    float v = -INFINITY;
-    int id = INT_MAX, rank = tid;
-    if (tid < C) {
-        v = ev[tid];
-        id = ei[tid];
-        rank = 0;
-        for (int k = 0; k < C; ++k) rank += ev[k] > v || (ev[k] == v && ei[k] < id);
-    }
-    if (rank < p.K) {
-        if (p.parts > 1) {
-            p.part_vals[((size_t)n * p.parts + part) * p.K + rank] = v;
-            p.part_ids[((size_t)n * p.parts + part) * p.K + rank] = id;
-        } else {
-            write_alternative(p, n, rank, st, v, id);
-        }
-    }
+    last.write(p, n, part, row.p, M);
 }
 
-// Joins the parts of a row: one workgroup of two wavefronts, one for the alternatives and one for the tokens.
+// A row of any length, in steps.  A lane keeps the place of its largest granule and the maximum of the others: behind the pass
+// the lanes whose largest reaches tau read that granule again, and the few of which another does, all of theirs.
 template <typename E>
-__global__ __launch_bounds__(2 * kWave) void logprobs_join_kernel(LogprobsParams p) {
-    const int n = blockIdx.x, lane = threadIdx.x & (kWave - 1);
-    const E *row = static_cast<const E *>(p.logits) + (long long)n * p.stride;
-    __shared__ float lv[kMaxParts][SPECEE_TOP_MAX];
-    __shared__ int li[kMaxParts][SPECEE_TOP_MAX];
-    for (int e = threadIdx.x; e < p.parts * p.K; e += blockDim.x) {
-        lv[e / p.K][e % p.K] = p.part_vals[(size_t)n * p.parts * p.K + e];
-        li[e / p.K][e % p.K] = p.part_ids[(size_t)n * p.parts * p.K + e];
+__global__ __launch_bounds__(kT) void logprobs_kernel(LogprobsParams p) {
+    constexpr int G = Granule<E>::n, GROUPS = kT / 16;
+    const int n = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
+    const E *body = row.p + row.head, *end = row.p + p.V - row.tail;
+    __shared__ float groups[GROUPS], tau;
+    __shared__ RowEnd<kWaves> last;
+
+    LaneSum<E> a(LaneSum<E>::kLowest);
+    float best = -INFINITY, others = -INFINITY;
+    int place = 0;
+    auto take = [&](const Granule<E> &x, int g) {
+        const float c = largest(x);
+        a.raise(c);
+#pragma unroll
+        for (int j = 0; j < G; ++j) a.add((float)x.v[j]);
+        others = fmaxf(others, fminf(c, best));
+        place = c > best ? g : place;
+        best = fmaxf(best, c);
+    };
+    int g = tid;
+    for (; g + (kUnroll - 1) * kT < row.whole; g += kUnroll * kT) {
+        Granule<E> x[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)(g + u * kT) * G);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) take(x[u], g + u * kT);
     }
-    float r = -INFINITY, s = 0.f, sx = 0.f;
+    for (; g < row.whole; g += kT) take(load_granule(body + (size_t)g * G), g);
+    const bool extra = tid < row.head + row.tail;
+    float xe = -INFINITY;
+    if (extra) {
+        xe = (float)(tid < row.head ? row.p[tid] : end[tid - row.head]);
+        a.raise(xe);
+        a.add(xe);
+    }
+    if (tid == 0) last.entries = 0;
+    float c = row16_max(fmaxf(best, xe == xe ? xe : -INFINITY));
+    if ((lane & 15) == 0) groups[tid / 16] = c;
+    __syncthreads();
+    c = lane < GROUPS ? groups[lane] : -INFINITY;
+    const float M = wave_max(c);
+    if (p.K) kth_largest<GROUPS, kWaves>(c, p.K, &tau);
+    a.move(M);
+    TopList top;
+    if (p.K) {
+        __syncthreads();
+        const float least = tau;
+        top.scan<1>(&xe, xe, tid < row.head ? tid : p.V - row.tail + tid - row.head, extra, least, p.K);
+        const bool several = others >= least && others > -INFINITY;
+        if (__ballot(best >= least && best > -INFINITY && !several)) {
+            Granule<E> x = {};
+            if (best >= least && !several && row.whole > 0) x = load_granule(body + (size_t)place * G);
+            top.scan<G>(x.v, best, row.index(place), !several, least, p.K);
+        }
+        unsigned long long who = __ballot(several);
+        const int steps = (row.whole + kT - 1) / kT;
+        while (who) {
+            const int l = __ffsll(who) - 1;
+            who &= who - 1;
+            for (int i0 = 0; i0 < steps; i0 += kWave) {
+                const int gi = (i0 + lane) * kT + (tid - lane) + l;
+                const bool has = gi < row.whole;
+                const Granule<E> x = load_granule(body + (size_t)(has ? gi : 0) * G);
+                top.scan<G>(x.v, largest(x), row.index(gi), has, least, p.K);
+            }
+        }
+    }
+    last.leave(a.s, a.st, top, p.K);
+    __syncthreads();
+    last.write(p, n, 0, row.p, M);
+}
+
+// Joins the parts of a row
+constexpr int kJoinWaves = 8;
+template <typename E>
+__global__ __launch_bounds__(kJoinWaves * kWave) void logprobs_join_kernel(LogprobsParams p) {
+    const int n = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1);
+    const E *row = static_cast<const E *>(p.logits) + (long long)n * p.stride;
+    __shared__ float v[kMaxParts * SPECEE_TOP_MAX];
+    __shared__ int id[kMaxParts * SPECEE_TOP_MAX];
+    const int C = p.parts * p.K;  // (at most one entry per thread; places without one hold -inf and INT_MAX)
+    if (tid < C) {
+        v[tid] = p.part_vals[(size_t)n * C + tid];
+        id[tid] = p.part_ids[(size_t)n * C + tid];
+    }
+    float r = -INFINITY;
+    LaneSum<E> a(0.f);
     if (lane < p.parts) {
         const float *sums = p.part_sums + ((size_t)n * p.parts + lane) * 4;
         r = sums[0];
-        s = sums[1];
-        sx = sums[2];
+        a.about(r);
+        a.s = sums[1];
+        a.st = sums[2];
     }
     const float M = wave_max(r);
-    shift(r, s, sx, M);
-    const RowStats st(M, wave_sum(s), wave_sum(sx));
+    a.move(M);
+    const RowStats st(M, wave_sum(a.s), wave_sum(a.st), LaneSum<E>::kMixed);
+    if (tid == 0) write_row(p, n, st);
+    write_tokens(p, n, row, st, tid);
+    if (p.K == 0) return;
     __syncthreads();
-    if (threadIdx.x >= kWave) {
-        if (lane == 0) write_row(p, n, st);
-        write_tokens(p, n, row, st, lane);
-        return;
-    }
-    // the parts' lists are sorted: the best of their first entries, K times
-    float mv = -INFINITY;
-    int mi = INT_MAX, at = 0;
-    for (int k = 0; k < p.K; ++k) {
-        const bool has = lane < p.parts && at < p.K;
-        float v = has ? lv[lane][at] : -INFINITY;
-        int id = has ? li[lane][at] : INT_MAX;
-        const int mine = id;
-        row16_argmax(v, id);
-        if (mine == id && mine != INT_MAX) ++at;
-        // (lanes of row 0 hold the parts; the winner is read from its first lane)
-        v = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
-        id = __builtin_amdgcn_readfirstlane(id);
-        if (lane == k) {
-            mv = v;
-            mi = id;
-        }
-    }
-    if (lane < p.K) write_alternative(p, n, lane, st, mv, mi);
+    int real = 0;
+    for (int o = 0; o < C; o += kWave) real += __popcll(__ballot(o + lane < C && v[min(o + lane, C - 1)] > -INFINITY));
+    if (tid >= real && tid < p.K) write_alternative(p, n, tid, st, -INFINITY, INT_MAX);
+    rank_entries<kJoinWaves>(v, id, C, p.K, [&](int k, float x, int i) {
+        if (x > -INFINITY) write_alternative(p, n, k, st, x, i);
+    });
 }
 
 // Gradient: elementwise, one workgroup per kGradSteps * 512 granules of a row; the ids that fall into its share are looked
@@ -395,7 +509,7 @@ constexpr int kGradSteps = 4;
 struct GradRow {
     float m, log_sum, entropy, factor, g_entropy;
     __device__ __forceinline__ float operator()(float x) const {
-        const float lp = fmaxf((x - m) - log_sum, kFloor);
+        const float lp = fmaxf((x - m) - log_sum, -200.f);  // exp(-200) is 0
         return -__builtin_amdgcn_exp2f(lp * kLog2e) * fmaf(g_entropy, lp + entropy, factor);
     }
 };
@@ -490,27 +604,58 @@ __global__ __launch_bounds__(kT) void logprobs_grad_kernel(LogprobsGradParams p)
 
 }  // namespace
 
-// Parts of a row: as many workgroups as make two per CU, as long as each has a granule for every thread
+// How rows are dealt out.  A workgroup of 512 or 1024 threads holds up to 8 granules per thread, 64 or 128 KB of logits: rows
+// that fit are held, which reads them once and looks at the alternatives in registers.  Longer rows are cut into parts that
+// fit as long as there are few of them (the parts of a row are joined by a second launch), and read in steps where there
+// are enough rows for the GPU without.
+namespace {
+struct Deal {
+    int parts, threads, granules;  // granules per thread; 0: in steps
+};
+Deal deal(int N, int V, bool half) {
+    const int whole = V / (half ? 8 : 4) + 1;
+    Deal d{1, 512, 0};
+    if (whole > 8 * 1024) {
+        if (N >= 512) return d;
+        d.parts = (whole + 8 * 512 - 1) / (8 * 512);
+        const int more = 512 / (N > 0 ? N : 1);
+        if (more > d.parts) d.parts = more;
+        if (d.parts > kMaxParts) d.parts = kMaxParts;
+    }
+    const int share = (whole + d.parts - 1) / d.parts + 1;
+    if (half && N >= 512) return Deal{1, 512, 0};
+    d.threads = share > 4 * 512 && share <= 8 * 1024 && (share > 8 * 512 || N < 128) ? 1024 : 512;
+    d.granules = (share + d.threads - 1) / d.threads;
+    if (d.granules > 8) return Deal{1, 512, 0};  // (a row that sixteen parts do not hold)
+    return d;
+}
+template <typename E>
+hipError_t launch_rows(const LogprobsParams &p, const Deal &d, hipStream_t s) {
+    const dim3 grid((unsigned)p.N * p.parts), threads(d.threads);
+    if (d.granules == 0)
+        hipLaunchKernelGGL(logprobs_kernel<E>, grid, threads, 0, s, p);
+    else if (d.threads == 1024 && d.granules <= 4)
+        hipLaunchKernelGGL((logprobs_held_kernel<E, 1024, 4>), grid, threads, 0, s, p);
+    else if (d.threads == 1024)
+        hipLaunchKernelGGL((logprobs_held_kernel<E, 1024, 8>), grid, threads, 0, s, p);
+    else if (d.granules <= 2)
+        hipLaunchKernelGGL((logprobs_held_kernel<E, 512, 2>), grid, threads, 0, s, p);
+    else if (d.granules <= 4)
+        hipLaunchKernelGGL((logprobs_held_kernel<E, 512, 4>), grid, threads, 0, s, p);
+    else
+        hipLaunchKernelGGL((logprobs_held_kernel<E, 512, 8>), grid, threads, 0, s, p);
+    if (p.parts > 1) hipLaunchKernelGGL(logprobs_join_kernel<E>, dim3(p.N), dim3(kJoinWaves * kWave), 0, s, p);
+    return hipGetLastError();
+}
+}  // namespace
+
 int logprobs_parts(int N, int V, bool half) {
-    const int whole = V / (half ? 8 : 4);
-    int parts = 512 / (N > 0 ? N : 1);
-    if (parts > whole / kT) parts = whole / kT;
-    return parts < 1 ? 1 : parts > kMaxParts ? kMaxParts : parts;
+    return deal(N, V, half).parts;
 }
 
 hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s) {
-    const dim3 grid((unsigned)p.N * p.parts);
-    if (half)
-        hipLaunchKernelGGL(logprobs_kernel<half_t>, grid, dim3(kT), 0, s, p);
-    else
-        hipLaunchKernelGGL(logprobs_kernel<float>, grid, dim3(kT), 0, s, p);
-    if (p.parts > 1) {
-        if (half)
-            hipLaunchKernelGGL(logprobs_join_kernel<half_t>, dim3(p.N), dim3(2 * kWave), 0, s, p);
-        else
-            hipLaunchKernelGGL(logprobs_join_kernel<float>, dim3(p.N), dim3(2 * kWave), 0, s, p);
-    }
-    return hipGetLastError();
+    const Deal d = deal(p.N, p.V, half);
+    return half ? launch_rows<half_t>(p, d, s) : launch_rows<float>(p, d, s);
 }
 
 hipError_t launch_logprobs_grad(const LogprobsGradParams &p, bool half, hipStream_t s) {
