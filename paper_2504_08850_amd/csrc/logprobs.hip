@@ -623,7 +623,7 @@ Deal deal(int N, int V, bool half) {
         if (d.parts > kMaxParts) d.parts = kMaxParts;
     }
     const int share = (whole + d.parts - 1) / d.parts + 1;
-    if (half && N >= 512) return Deal{1, 512, 0};
+    if (N >= 512) return Deal{1, 512, 0};
     d.threads = share > 4 * 512 && share <= 8 * 1024 && (share > 8 * 512 || N < 128) ? 1024 : 512;
     d.granules = (share + d.threads - 1) / d.threads;
     if (d.granules > 8) return Deal{1, 512, 0};  // (a row that sixteen parts do not hold)

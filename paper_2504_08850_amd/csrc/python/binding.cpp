@@ -13,6 +13,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/version.h>
@@ -202,6 +203,59 @@ PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
     return checked(F, args, n);
 }
 
+// expect(tensor, kind, rows, columns, ...): each tensor (None passes) is of that type (0 fp16, 1 fp32, 2 int32, 3 e4m3) and
+// size ([rows] where columns is -1) and on the current device, the one that the library launches on.  The sizes that a call
+// derives from one tensor are held against all others here: 0.1 us a tensor, four times that in Python.
+PyObject *expect(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    static const c10::ScalarType kinds[4] = {c10::ScalarType::Half, c10::ScalarType::Float, c10::ScalarType::Int,
+                                             c10::ScalarType::Float8_e4m3fn};
+    if (n % 4) {
+        PyErr_SetString(PyExc_TypeError, "tensor, kind, rows, columns are expected");
+        return nullptr;
+    }
+    try {
+        const int device = c10::hip::current_device();
+        for (Py_ssize_t i = 0; i < n; i += 4) {
+            if (args[i] == Py_None) continue;
+            if (!THPVariable_Check(args[i])) {
+                PyErr_Format(PyExc_TypeError, "a tensor is expected, not %s", Py_TYPE(args[i])->tp_name);
+                return nullptr;
+            }
+            long long v[3];
+            for (int k = 0; k < 3; ++k) {
+                v[k] = PyLong_AsLongLong(args[i + 1 + k]);
+                if (v[k] == -1 && PyErr_Occurred()) return nullptr;
+            }
+            if (v[0] < 0 || v[0] > 3) {
+                PyErr_SetString(PyExc_TypeError, "unknown kind");
+                return nullptr;
+            }
+            const at::Tensor &t = THPVariable_Unpack(args[i]);
+            if (!t.is_cuda() || t.get_device() != device) {
+                PyErr_SetString(PyExc_AssertionError, "a tensor is not on the current device");
+                return nullptr;
+            }
+            if (t.scalar_type() != kinds[v[0]]) {
+                PyErr_Format(PyExc_AssertionError, "a tensor of type %s is expected, not %s", c10::toString(kinds[v[0]]),
+                             c10::toString(t.scalar_type()));
+                return nullptr;
+            }
+            const bool vec = v[2] < 0;
+            if (t.dim() != (vec ? 1 : 2) || t.size(0) != v[1] || (!vec && t.size(1) != v[2])) {
+                if (vec)
+                    PyErr_Format(PyExc_AssertionError, "a tensor of size [%lld] is expected", v[1]);
+                else
+                    PyErr_Format(PyExc_AssertionError, "a tensor of size [%lld][%lld] is expected", v[1], v[2]);
+                return nullptr;
+            }
+        }
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+    Py_RETURN_NONE;
+}
+
 #define SPECEE_ENTRY(name) {#name, reinterpret_cast<PyCFunction>(&entry<&name>), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {
     SPECEE_ENTRY(specee_predict),        SPECEE_ENTRY(specee_predict_q4),
@@ -212,6 +266,7 @@ PyMethodDef methods[] = {
     SPECEE_ENTRY(specee_layer_loop),     SPECEE_ENTRY(specee_layer_loop_q4),
     SPECEE_ENTRY(specee_block_norm),     SPECEE_ENTRY(specee_logprobs),
     SPECEE_ENTRY(specee_logprobs_grad),  SPECEE_ENTRY(specee_matmul_f8),
+    {"expect", reinterpret_cast<PyCFunction>(&expect), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", "Argument marshalling of libspecee.so", -1, methods,

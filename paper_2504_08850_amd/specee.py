@@ -407,11 +407,7 @@ def predict_tree_q4(hidden, gamma, qweight, scales, zeros, group, ids, prev_prob
     return out
 
 
-def _here(t):
-    """The library launches on the current device: a tensor of another one is refused."""
-    assert t.is_cuda, "device-resident tensors only"
-    assert t.get_device() == torch.cuda.current_device(), "the tensors' device has to be the current one"
-    return t.device
+F16, F32, I32, F8 = range(4)  # kinds of _call().expect
 
 
 def block_norm(hidden, gamma=None, branch=None, gamma_post=None, gate=None, hidden_scale=1.0, branch_scale=1.0, eps=1e-5,
@@ -420,31 +416,29 @@ def block_norm(hidden, gamma=None, branch=None, gamma_post=None, gate=None, hidd
     gamma.  gate [d] or [1][d] (all rows) or [N][d].  Returns dict(hidden) with x (fp16) if want_x, x8 (float8_e4m3fn)
     and x8_scales [N][ceil(d/128)] if want_f8; out: such a dict, whose hidden may be `hidden` itself."""
     N, d = hidden.shape
-    dev = _here(hidden)
+    blocks = (d + 127) // 128
     if gamma is None:
         want_x = want_f8 = False
     gate_rows = 0
     if gate is not None:
         gate_rows = 1 if gate.dim() == 1 else gate.shape[0]
-        assert gate.shape[-1] == d and gate_rows in (1, N), (gate.shape, hidden.shape)
-    assert branch is None or branch.shape == hidden.shape, (branch.shape, hidden.shape)
-    assert all(g is None or g.shape == (d,) for g in (gamma, gamma_post)), "norm weights are [d]"
+        assert gate_rows in (1, N), (gate.shape, hidden.shape)
     if out is None:
         out = dict(hidden=torch.empty_like(hidden))
         if want_x:
             out["x"] = torch.empty_like(hidden)
         if want_f8:
-            out["x8"] = torch.empty((N, d), dtype=torch.float8_e4m3fn, device=dev)
-            out["x8_scales"] = torch.empty((N, (d + 127) // 128), dtype=torch.float32, device=dev)
-    x, x8, scales = (out["x"] if want_x else None), None, None
-    if want_f8:
-        x8, scales = out["x8"], out["x8_scales"]
-        assert x8.dtype == torch.float8_e4m3fn and x8.shape == (N, d), (x8.dtype, x8.shape)
-        assert scales.dtype == torch.float32 and scales.shape == (N, (d + 127) // 128), (scales.dtype, scales.shape)
-    for t in (out["hidden"], x):
-        assert t is None or (t.dtype == torch.float16 and t.shape == hidden.shape), (t.dtype, t.shape)
-    rc = _call().specee_block_norm((d, 1, 1, 1, eps, 0.5), N, hidden, branch, gamma_post, gate, gate_rows, hidden_scale,
-                                   branch_scale, gamma, out["hidden"], x, x8, scales, _handle(stream))
+            out["x8"] = torch.empty((N, d), dtype=torch.float8_e4m3fn, device=hidden.device)
+            out["x8_scales"] = torch.empty((N, blocks), dtype=torch.float32, device=hidden.device)
+    new = out["hidden"]
+    x = out["x"] if want_x else None
+    x8, scales = (out["x8"], out["x8_scales"]) if want_f8 else (None, None)
+    call = _call()
+    call.expect(hidden, F16, N, d, branch, F16, N, d, gamma, F16, d, -1, gamma_post, F16, d, -1, new, F16, N, d,
+                x, F16, N, d, x8, F8, N, d, scales, F32, N, blocks,
+                gate, F16, *((d, -1) if gate_rows and gate.dim() == 1 else (gate_rows, d)))
+    rc = call.specee_block_norm((d, 1, 1, 1, eps, 0.5), N, hidden, branch, gamma_post, gate, gate_rows, hidden_scale,
+                                branch_scale, gamma, new, x, x8, scales, _handle(stream))
     if rc:
         raise SpeceeError("specee_block_norm", rc)
     return out
@@ -455,48 +449,46 @@ def matmul_f8(x, x_scales, weight, w_scales, dtype=torch.float32, out=None, work
     [ceil(V/128)][ceil(d/128)] fp32; returns dict(out) with out [N][V] of `dtype`, fp32 or fp16."""
     N, d = x.shape
     V = weight.shape[0]
-    dev = _here(x)
-    nb = (d + 127) // 128
-    assert weight.shape[1] == d and x_scales.shape == (N, nb) and w_scales.shape == ((V + 127) // 128, nb), \
-        (x.shape, x_scales.shape, weight.shape, w_scales.shape)
+    blocks = (d + 127) // 128
+    assert dtype in (torch.float32, torch.float16), dtype
     if out is None:
-        out = torch.empty((N, V), dtype=dtype, device=dev)
-    assert out.dtype in (torch.float32, torch.float16) and out.dtype == dtype and out.shape == (N, V), (out.dtype, out.shape)
-    dims = (d, V, 1, 1, 0.0, 0.5)
-    workspace, wbytes = _workspace(OP_MATMUL_F8, dims, N, 0, workspace, dev)
+        out = torch.empty((N, V), dtype=dtype, device=x.device)
     f32, f16 = (out, None) if dtype == torch.float32 else (None, out)
-    rc = _call().specee_matmul_f8(dims, N, x, x_scales, weight, w_scales, f32, f16, workspace, wbytes, _handle(stream))
+    call = _call()
+    call.expect(x, F8, N, d, weight, F8, V, d, x_scales, F32, N, blocks, w_scales, F32, (V + 127) // 128, blocks,
+                f32, F32, N, V, f16, F16, N, V)
+    dims = (d, V, 1, 1, 0.0, 0.5)
+    workspace, wbytes = _workspace(OP_MATMUL_F8, dims, N, 0, workspace, x.device)
+    rc = call.specee_matmul_f8(dims, N, x, x_scales, weight, w_scales, f32, f16, workspace, wbytes, _handle(stream))
     if rc:
         raise SpeceeError("specee_matmul_f8", rc)
     return dict(out=out, _workspace=workspace)
 
 
 def _rows(t):
-    """(flat view, stride) of rows of which each is contiguous; the view reaches from the first to the last element."""
+    """(fp32, fp16, stride): one of the two is a flat view from the first to the last element of the rows of t, which may be
+    apart, the other None."""
     N, V = t.shape
     if t.is_contiguous():
-        return t, V
-    assert t.stride(1) == 1 or V == 1, "the elements of a row have to be contiguous"
-    stride = t.stride(0) if N > 1 else V
-    assert stride >= V, "rows that overlap"
-    return t.as_strided(((N - 1) * stride + V,), (1,)), stride
-
-
-def _logits(t):
-    """(fp32, fp16, stride): one of the two is the logits' rows, the other None."""
-    flat, stride = _rows(t)
-    assert t.dtype in (torch.float32, torch.float16), t.dtype
-    return (flat, None, stride) if t.dtype == torch.float32 else (None, flat, stride)
+        flat, stride = t, V
+    else:
+        assert t.stride(1) == 1 or V == 1, "the elements of a row have to be contiguous"
+        stride = t.stride(0) if N > 1 else V
+        assert stride >= V, "rows that overlap"
+        flat = t.as_strided(((N - 1) * stride + V,), (1,))
+    if t.dtype == torch.float32:
+        return flat, None, stride
+    assert t.dtype == torch.float16, t.dtype
+    return None, flat, stride
 
 
 def logprobs(logits, ids=None, n_top=0, out=None, workspace=None, stream=None):
     """specee_logprobs: logits [N][V] fp32 or fp16 (rows may be apart), ids [N][T].  Returns dict(max_logit, log_sum,
     entropy) with logprobs [N][T] if ids are given, top_ids and top_logprobs [N][n_top] if n_top."""
     N, V = logits.shape
-    dev = _here(logits)
-    f32, f16, stride = _logits(logits)
+    f32, f16, stride = _rows(logits)
     T = 0 if ids is None else ids.shape[1]
-    assert ids is None or ids.shape[0] == N, (ids.shape, logits.shape)
+    dev = logits.device
     if out is None:
         new = lambda *shape: torch.empty(shape, dtype=torch.float32, device=dev)
         out = dict(max_logit=new(N), log_sum=new(N), entropy=new(N))
@@ -505,18 +497,16 @@ def logprobs(logits, ids=None, n_top=0, out=None, workspace=None, stream=None):
         if n_top:
             out["top_ids"] = torch.empty((N, n_top), dtype=torch.int32, device=dev)
             out["top_logprobs"] = new(N, n_top)
-    for k, shape in (("max_logit", (N,)), ("log_sum", (N,)), ("entropy", (N,)), ("logprobs", (N, T)),
-                     ("top_logprobs", (N, n_top))):
-        if shape[-1] or N == 0:
-            t = out.get(k) if k in ("max_logit", "log_sum", "entropy") else out[k] if shape[-1] else None
-            assert t is None or (t.dtype == torch.float32 and t.shape == shape), (k, t.dtype, t.shape)
+    m, log_sum, entropy = out["max_logit"], out["log_sum"], out["entropy"]
+    lp = out["logprobs"] if T else None
+    top_ids, top_lp = (out["top_ids"], out["top_logprobs"]) if n_top else (None, None)
+    call = _call()
+    call.expect(logits, F16 if f32 is None else F32, N, V, ids, I32, N, T, lp, F32, N, T, m, F32, N, -1, log_sum, F32, N, -1,
+                entropy, F32, N, -1, top_ids, I32, N, n_top, top_lp, F32, N, n_top)
     dims = (8, V, 1, 1, 0.0, 0.5)
     workspace, wbytes = _workspace(OP_LOGPROBS, dims, N, n_top, workspace, dev)
-    top_ids = out["top_ids"] if n_top else None
-    assert top_ids is None or (top_ids.dtype == torch.int32 and top_ids.shape == (N, n_top)), top_ids.shape
-    rc = _call().specee_logprobs(dims, N, f32, f16, stride, ids if T else None, T, n_top, out["logprobs"] if T else None,
-                                 out.get("max_logit"), out.get("log_sum"), out.get("entropy"), top_ids,
-                                 out["top_logprobs"] if n_top else None, workspace, wbytes, _handle(stream))
+    rc = call.specee_logprobs(dims, N, f32, f16, stride, ids if T else None, T, n_top, lp, m, log_sum, entropy, top_ids,
+                              top_lp, workspace, wbytes, _handle(stream))
     if rc:
         raise SpeceeError("specee_logprobs", rc)
     out["_workspace"] = workspace
@@ -527,18 +517,18 @@ def logprobs_grad(logits, ids, max_logit, log_sum, entropy=None, g_logprobs=None
     """specee_logprobs_grad: gradient of the logits of `logprobs`, whose max_logit, log_sum (and entropy, with g_entropy)
     are given, from those of its log probabilities [N][T] and entropies [N].  `out` may be the logits themselves."""
     N, V = logits.shape
-    _here(logits)
-    f32, f16, stride = _logits(logits)
+    f32, f16, stride = _rows(logits)
     T = 0 if ids is None else ids.shape[1]
-    assert ids is None or (ids.shape[0] == N and g_logprobs is not None and g_logprobs.shape == ids.shape), "g_logprobs"
-    assert all(t is None or t.shape == (N,) for t in (max_logit, log_sum, entropy, g_entropy)), "one value per row"
+    assert not T or g_logprobs is not None, "ids come with g_logprobs"
     if out is None:
         out = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
-    assert out.dtype == logits.dtype and out.shape == logits.shape, (out.dtype, out.shape)
-    g32, g16, gstride = _logits(out)
-    rc = _call().specee_logprobs_grad((8, V, 1, 1, 0.0, 0.5), N, f32, f16, stride, ids if T else None, T, max_logit,
-                                      log_sum, entropy, g_logprobs if T else None, g_entropy, g32, g16, gstride,
-                                      _handle(stream))
+    g32, g16, gstride = _rows(out)
+    call = _call()
+    kind = F16 if f32 is None else F32
+    call.expect(logits, kind, N, V, out, kind, N, V, ids, I32, N, T, g_logprobs, F32, N, T, max_logit, F32, N, -1,
+                log_sum, F32, N, -1, entropy, F32, N, -1, g_entropy, F32, N, -1)
+    rc = call.specee_logprobs_grad((8, V, 1, 1, 0.0, 0.5), N, f32, f16, stride, ids if T else None, T, max_logit, log_sum,
+                                   entropy, g_logprobs if T else None, g_entropy, g32, g16, gstride, _handle(stream))
     if rc:
         raise SpeceeError("specee_logprobs_grad", rc)
     return out

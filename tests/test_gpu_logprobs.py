@@ -361,7 +361,7 @@ def test_refusals_without_a_gpu(sp):
     assert call(tid=None) == -1 and call(tlp=None) == -1
     assert call(x=odd) == -2 and call(x=None, h=odd) == -2
     assert call(N=0, x=None) == 0
-    big = dict(V=32000, stride=32000)                                  # one row in parts: a workspace is needed
+    big = dict(V=128256, stride=128256)                                # one row in parts: a workspace is needed
     assert call(**big, ws=None, n=0) == -3 and call(**big, n=16) == -3 and call(**big, ws=C.c_void_p(0x1004)) == -2
 
     def grad(V=100, N=1, x=a, h=None, stride=100, ids=a, T=1, m=a, s=a, H=a, g=a, gh=None, o=b, oh=None, ostride=100):
