@@ -72,6 +72,10 @@ __device__ __forceinline__ void store_quad(T *out, size_t at, int left, const fl
 __device__ __forceinline__ void load_lds16(uint32_t lds, uint32_t off, const void *base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
+// (for what is read once)
+__device__ __forceinline__ void load_lds16_once(uint32_t lds, uint32_t off, const void *base) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt" ::"s"(lds), "v"(off), "s"(base) : "memory");
+}
 __device__ __forceinline__ void load_lds4(uint32_t lds, uint32_t off, const void *base) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
 }
@@ -81,32 +85,38 @@ __device__ __forceinline__ void landed() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
-// A workgroup's tile: WV wavefronts of 128 rows of w by 4 of NJ * 16 rows of x
-template <int WV, int NJ>
+__device__ __forceinline__ void meet() {
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// A workgroup's tile: WV by WN wavefronts, each with I * 16 rows of w by J * 16 of x
+template <int WV_, int WN_, int I_, int J_>
 struct Tile {
-    static constexpr int waves = WV * 4, threads = waves * kWave;
-    static constexpr int rows = WV * 128, states = NJ * 64;
-    static constexpr int w_bytes = rows * kBlock, x_bytes = states * kBlock;
-    static constexpr int buffer = w_bytes + x_bytes + states * 4;  // of one block
+    static constexpr int WV = WV_, WN = WN_, I = I_, J = J_;
+    static constexpr int waves = WV * WN, threads = waves * kWave;
+    static constexpr int rows = WV * I * 16, states = WN * J * 16;
+    static constexpr int w_bytes = rows * kBlock, x_bytes = states * kBlock, groups = (states + 63) / 64;
+    static constexpr int buffer = w_bytes + x_bytes + groups * 256;  // of one block, with the scales of x
     static constexpr int buffers = 3 * buffer <= 156 * 1024 ? 3 : 2;
     static constexpr int w_loads = rows / 8 / waves, x_loads = states / 8 / waves;  // of a wavefront, 8 rows each
     static constexpr int loads = w_loads + x_loads + 1;
+    static_assert(w_loads * waves * 8 == rows && x_loads * waves * 8 == states && 128 % (I * 16) == 0, "");
 };
 
 // Brings one block of a workgroup's tile to LDS.  A load brings eight rows, a row's eight pieces of 16 bytes in the order
 // piece ^ (row % 8): the 16 rows that the lanes of an operand read then lie in different banks.
-template <int WV, int NJ>
+template <typename S>
 struct Loader {
-    using S = Tile<WV, NJ>;
     const uint8_t *wbase, *xbase;
     const float *sbase;
     uint32_t woff[S::w_loads], xoff[S::x_loads], soff;
     uint32_t lds0;
     int d, piece, wave, lane;
+    bool once;  // whether this workgroup alone reads these rows of w
     unsigned char *smem;
 
     __device__ __forceinline__ Loader(const MatmulF8Params &p, int v0, int n0, int wave_, int lane_, unsigned char *smem_)
-        : d(p.d), wave(wave_), lane(lane_), smem(smem_) {
+        : d(p.d), wave(wave_), lane(lane_), once(gridDim.y == 1), smem(smem_) {
         lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
         const int sub = lane >> 3;
         piece = ((lane & 7) ^ sub) * 16;
@@ -120,41 +130,53 @@ struct Loader {
             xoff[i] = (uint32_t)min((wave * S::x_loads + i) * 8 + sub, p.N - 1 - n0) * (uint32_t)p.d + piece;
         // (a scale is loaded by every wavefront that has none of its own to load)
         sbase = p.xs + (size_t)n0 * p.blocks;
-        soff = (uint32_t)min((wave % NJ) * 64 + lane, p.N - 1 - n0) * (uint32_t)p.blocks * 4;
+        soff = (uint32_t)min((wave % S::groups) * 64 + lane, p.N - 1 - n0) * (uint32_t)p.blocks * 4;
     }
-    __device__ __forceinline__ void operator()(int b, int slot) const {
-        const uint32_t at = lds0 + slot * S::buffer;
+    // Rows behind their ends hold zeros: a last block may be shorter
+    template <int LOADS>
+    __device__ __forceinline__ void short_block(int b, unsigned char *to, const uint8_t *base, const uint32_t (&off)[LOADS]) const {
         const int k0 = b * kBlock;
-        if (k0 + kBlock <= d) {
+        const bool in = k0 + piece < d;
+        uintx4 *dst = reinterpret_cast<uintx4 *>(to) + lane;
 #pragma unroll
-            for (int i = 0; i < S::w_loads; ++i) load_lds16(at + (wave * S::w_loads + i) * 1024, woff[i], wbase + k0);
-#pragma unroll
-            for (int i = 0; i < S::x_loads; ++i)
-                load_lds16(at + S::w_bytes + (wave * S::x_loads + i) * 1024, xoff[i], xbase + k0);
-        } else {  // a last block that is shorter: zeros behind the rows' ends
-            const bool in = k0 + piece < d;
-            uintx4 *dst = reinterpret_cast<uintx4 *>(smem + slot * S::buffer) + lane;
-#pragma unroll
-            for (int i = 0; i < S::w_loads; ++i) {
-                uintx4 v = *reinterpret_cast<const uintx4 *>(wbase + (in ? k0 + woff[i] : 0u));
-                if (!in) v = uintx4{0, 0, 0, 0};
-                dst[(wave * S::w_loads + i) * 64] = v;
-            }
-#pragma unroll
-            for (int i = 0; i < S::x_loads; ++i) {
-                uintx4 v = *reinterpret_cast<const uintx4 *>(xbase + (in ? k0 + xoff[i] : 0u));
-                if (!in) v = uintx4{0, 0, 0, 0};
-                dst[S::w_bytes / 16 + (wave * S::x_loads + i) * 64] = v;
-            }
+        for (int i = 0; i < LOADS; ++i) {
+            uintx4 v = *reinterpret_cast<const uintx4 *>(base + (in ? k0 + off[i] : 0u));
+            if (!in) v = uintx4{0, 0, 0, 0};
+            dst[(wave * LOADS + i) * 64] = v;
         }
-        load_lds4(at + S::w_bytes + S::x_bytes + (wave % NJ) * 256, soff, sbase + b);
+    }
+    __device__ __forceinline__ void load_w(int b, int slot) const {
+        const int k0 = b * kBlock;
+        if (k0 + kBlock > d) {
+            short_block(b, smem + slot * S::buffer, wbase, woff);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < S::w_loads; ++i) {
+            const uint32_t to = lds0 + slot * S::buffer + (wave * S::w_loads + i) * 1024;
+            if (once)
+                load_lds16_once(to, woff[i], wbase + k0);
+            else
+                load_lds16(to, woff[i], wbase + k0);
+        }
+    }
+    __device__ __forceinline__ void load_x(int b, int slot) const {
+        const int k0 = b * kBlock;
+        const uint32_t at = lds0 + slot * S::buffer + S::w_bytes;
+        if (k0 + kBlock > d) {
+            short_block(b, smem + slot * S::buffer + S::w_bytes, xbase, xoff);
+        } else {
+#pragma unroll
+            for (int i = 0; i < S::x_loads; ++i) load_lds16(at + (wave * S::x_loads + i) * 1024, xoff[i], xbase + k0);
+        }
+        load_lds4(at + S::x_bytes + (wave % S::groups) * 256, soff, sbase + b);
     }
 };
 
 // The scales of 128 rows of w (a scalar load: a vector load would be waited for behind the tiles that are in flight)
 typedef const __attribute__((address_space(4))) float *scalar_ptr;
-__device__ __forceinline__ scalar_ptr row_scales(const MatmulF8Params &p, int v0, int wv) {
-    return (scalar_ptr)(uintptr_t)(p.ws + (size_t)min((v0 >> 7) + wv, (p.V - 1) >> 7) * p.blocks);
+__device__ __forceinline__ scalar_ptr row_scales(const MatmulF8Params &p, int v) {
+    return (scalar_ptr)(uintptr_t)(p.ws + (size_t)(min(v, p.V - 1) >> 7) * p.blocks);
 }
 
 __device__ __forceinline__ Codes read_codes(const unsigned char *t, int i, int frag) {
@@ -164,17 +186,17 @@ __device__ __forceinline__ Codes read_codes(const unsigned char *t, int i, int f
     return o;
 }
 
-template <typename T, int WV, int NJ>
-__device__ __forceinline__ void store_tile(const MatmulF8Params &p, const floatx4 (&acc)[8][NJ], int v0, int n0) {
+template <typename T, int I, int J>
+__device__ __forceinline__ void store_tile(const MatmulF8Params &p, const floatx4 (&acc)[I][J], int v0, int n0) {
     const bool parts = gridDim.z > 1;
     const int q = (threadIdx.x & 63) >> 4, c = threadIdx.x & 15;
     float *part = static_cast<float *>(p.workspace) + (size_t)blockIdx.z * p.N * p.V;
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
+    for (int j = 0; j < J; ++j) {
         const int n = n0 + j * 16 + c;
         if (n >= p.N) continue;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < I; ++i) {
             const int v = v0 + i * 16 + 4 * q;
             if (v >= p.V) continue;
             if (parts)
@@ -186,48 +208,78 @@ __device__ __forceinline__ void store_tile(const MatmulF8Params &p, const floatx
 }
 
 // T: type of the result.  fp16 results take the codes as they are, fp32 results as halves.
-template <typename T, int WV, int NJ>
-__global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p) {
-    using S = Tile<WV, NJ>;
+template <typename T, typename S>
+__global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params p) {
+    constexpr int I = S::I, J = S::J;
     typedef typename std::conditional<sizeof(T) == 4, Halves, Codes>::type Operand;
     extern __shared__ __attribute__((aligned(1024))) unsigned char f8_smem[];
     const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wv = wave >> 2, wn = wave & 3;
+    const int wv = wave / S::WN, wn = wave % S::WN;
     const int v0 = blockIdx.x * S::rows, n0 = blockIdx.y * S::states;
     const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
     const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
-    const Loader<WV, NJ> load(p, v0, n0, wave, lane, f8_smem);
+    const Loader<S> load(p, v0, n0, wave, lane, f8_smem);
 
-    floatx4 acc[8][NJ] = {};
+    floatx4 acc[I][J] = {};
     const int frag = c * kBlock + ((q ^ (c & 7)) << 4);
-    const scalar_ptr ws = row_scales(p, v0, wv);
+    const scalar_ptr ws = row_scales(p, v0 + wv * I * 16);
     float sw = ws[b0];
+    constexpr bool kTwo = S::buffers == 2;
 #pragma unroll
     for (int k = 0; k < S::buffers - 1; ++k)
-        if (b0 + k < b1) load(b0 + k, k);
-    for (int b = b0; b < b1; ++b) {
-        if (S::buffers == 3 && b + 1 < b1)
-            landed<S::loads>();
-        else
-            landed<0>();
-        if (b + S::buffers - 1 < b1) load(b + S::buffers - 1, (b - b0 + S::buffers - 1) % S::buffers);
-        const float sw_next = ws[min(b + 1, b1 - 1)];
-        const unsigned char *buf = f8_smem + ((b - b0) % S::buffers) * S::buffer;
-        const unsigned char *wt = buf + wv * 128 * kBlock, *xt = buf + S::w_bytes + wn * NJ * 16 * kBlock;
-        const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * NJ * 16 + c;
-        float s[NJ];
-        Operand x[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            x[j] = Operand(read_codes(xt, j, frag));
-            s[j] = st[j * 16] * sw;
+        if (b0 + k < b1) {
+            load.load_x(b0 + k, k);
+            load.load_w(b0 + k, k);
         }
+    if (kTwo && b0 + 1 < b1) load.load_x(b0 + 1, 1);
+    for (int b = b0; b < b1; ++b) {
+        const int slot = (b - b0) % S::buffers;
+        if (b + 1 >= b1)
+            landed<0>();
+        else if (kTwo)
+            landed<S::x_loads + 1>();  // the next block's x may be on its way
+        else
+            landed<S::loads>();
+        const unsigned char *buf = f8_smem + slot * S::buffer;
+        const unsigned char *wt = buf + wv * I * 16 * kBlock, *xt = buf + S::w_bytes + wn * J * 16 * kBlock;
+        const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * J * 16 + c;
+        float s[J];
+        Operand x[J];
+        if (kTwo) {
+            // x is in registers once all have read it: its place is free for the block after the next
+            Codes xc[J];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+            for (int j = 0; j < J; ++j) {
+                xc[j] = read_codes(xt, j, frag);
+                s[j] = st[j * 16];
+            }
+            if (b + 1 < b1) load.load_w(b + 1, slot ^ 1);
+            meet();
+            if (b + 2 < b1) load.load_x(b + 2, slot);
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                x[j] = Operand(xc[j]);
+                s[j] *= sw;
+            }
+        } else {
+            const int ahead = b + S::buffers - 1;
+            if (ahead < b1) {
+                load.load_x(ahead, (ahead - b0) % S::buffers);
+                load.load_w(ahead, (ahead - b0) % S::buffers);
+            }
+#pragma unroll
+            for (int j = 0; j < J; ++j) {
+                x[j] = Operand(read_codes(xt, j, frag));
+                s[j] = st[j * 16] * sw;
+            }
+        }
+        const float sw_next = ws[min(b + 1, b1 - 1)];
+#pragma unroll
+        for (int i = 0; i < I; ++i) {
             const Operand w(read_codes(wt, i, frag));
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) {
+            for (int j = 0; j < J; ++j) {
                 const floatx4 t = block_product(w, x[j]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[j], t[e], acc[i][j][e]);
@@ -235,84 +287,7 @@ __global__ __launch_bounds__(WV * 256, 2) void matmul_f8_kernel(MatmulF8Params p
         }
         sw = sw_next;
     }
-    store_tile<T, WV, NJ>(p, acc, v0 + wv * 128, n0 + wn * NJ * 16);
-}
-
-__device__ __forceinline__ void meet() {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-}
-__device__ __forceinline__ void all_landed() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-}
-
-// The same with eight wavefronts, two on a SIMD, of which one reads a block's operands from LDS into registers while the
-// other multiplies: wavefronts 4..7 are half a block behind 0..3.  Phase 2b: 0..3 read block b, 4..7 multiply block b - 1;
-// phase 2b + 1: 0..3 multiply block b, 4..7 read it.  A phase begins with a meeting of all; behind the one of phase 2b, when
-// block b - 1 has been read by all, all ask for block b + 1 in its place, and wait for it before the meeting of phase 2b + 2.
-template <typename T, int NJ>
-__global__ __launch_bounds__(512, 2) void matmul_f8_turns_kernel(MatmulF8Params p) {
-    using S = Tile<2, NJ>;
-    typedef typename std::conditional<sizeof(T) == 4, Halves, Codes>::type Operand;
-    extern __shared__ __attribute__((aligned(1024))) unsigned char f8_smem[];
-    const int lane = threadIdx.x & 63, q = lane >> 4, c = lane & 15;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wv = wave >> 2, wn = wave & 3;
-    const int v0 = blockIdx.x * S::rows, n0 = blockIdx.y * S::states;
-    const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
-    const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
-    const Loader<2, NJ> load(p, v0, n0, wave, lane, f8_smem);
-
-    floatx4 acc[8][NJ] = {};
-    const int frag = c * kBlock + ((q ^ (c & 7)) << 4);
-    const scalar_ptr ws = row_scales(p, v0, wv);
-    load(b0, 0);
-    all_landed();
-    if (wv == 1) {
-        meet();
-        if (b0 + 1 < b1) load(b0 + 1, 1);
-    }
-    int slot = 0;
-    for (int b = b0; b < b1; ++b, slot ^= 1) {
-        meet();
-        if (wv == 0 && b + 1 < b1) load(b + 1, slot ^ 1);
-        const float sw = ws[b];
-        const unsigned char *buf = f8_smem + slot * S::buffer;
-        const unsigned char *wt = buf + wv * 128 * kBlock, *xt = buf + S::w_bytes + wn * NJ * 16 * kBlock;
-        const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * NJ * 16 + c;
-        Codes xc[NJ], wc[8];
-        float s[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            xc[j] = read_codes(xt, j, frag);
-            s[j] = st[j * 16];
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) wc[i] = read_codes(wt, i, frag);
-        if (wv == 1) all_landed();
-        meet();
-        if (wv == 1 && b + 2 < b1) load(b + 2, slot);
-        Operand x[NJ];
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) {
-            x[j] = Operand(xc[j]);
-            s[j] *= sw;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const Operand w(wc[i]);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) {
-                const floatx4 t = block_product(w, x[j]);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][j][e] = fmaf(s[j], t[e], acc[i][j][e]);
-            }
-        }
-        if (wv == 0) all_landed();
-    }
-    if (wv == 0) meet();
-    store_tile<T, 2, NJ>(p, acc, v0 + wv * 128, n0 + wn * NJ * 16);
+    store_tile<T, I, J>(p, acc, v0 + wv * I * 16, n0 + wn * J * 16);
 }
 
 // Sums of the parts, in their order
@@ -390,7 +365,7 @@ __global__ __launch_bounds__(1024) void matmul_f8_stream_kernel(MatmulF8Params p
 
     for (; unit < units; unit += gridDim.x) {
         const int next = min(unit + (int)gridDim.x, units - 1);
-        const scalar_ptr ws = row_scales(p, unit * 16 * unit_tiles, 0);
+        const scalar_ptr ws = row_scales(p, unit * 16 * unit_tiles);
         float f[CPW];
 #pragma unroll
         for (int k = 0; k < CPW; ++k) f[k] = sx[k] * ws[min(first + k, p.blocks - 1)];
@@ -438,26 +413,43 @@ __global__ __launch_bounds__(1024) void matmul_f8_stream_kernel(MatmulF8Params p
     }
 }
 
+// The tiles that there are, by their number in kTiles
+template <int K>
+struct TileOf;
+template <> struct TileOf<0> { using type = Tile<4, 1, 2, 2>; };
+template <> struct TileOf<1> { using type = Tile<4, 1, 2, 4>; };
+template <> struct TileOf<2> { using type = Tile<2, 2, 4, 4>; };
+template <> struct TileOf<3> { using type = Tile<1, 4, 8, 4>; };
+template <> struct TileOf<4> { using type = Tile<2, 4, 8, 2>; };
+template <> struct TileOf<5> { using type = Tile<2, 4, 8, 3>; };
+template <> struct TileOf<6> { using type = Tile<2, 4, 8, 4>; };
+template <> struct TileOf<7> { using type = Tile<2, 2, 4, 6>; };
+template <> struct TileOf<8> { using type = Tile<2, 2, 4, 2>; };
+template <> struct TileOf<9> { using type = Tile<4, 2, 4, 4>; };
+
 struct Shape {
-    int wv, nj, parts;
+    int tile, parts;  // tile -1: the stream for few states
 };
 
 Shape shape_of(int N, int V, int d) {
     const int blocks = (d + kBlock - 1) / kBlock;
-    if (N <= 16) return Shape{0, 0, (blocks + kStreamBlocks - 1) / kStreamBlocks};
-    Shape best{1, (N + 63) / 64 > 4 ? 4 : (N + 63) / 64, 1};
+    if (N <= 16) return Shape{-1, (blocks + kStreamBlocks - 1) / kStreamBlocks};
+    Shape best{N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 2 : 3, 1};
+    int rows = 128, states = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
     if (N > 256) {
         long cost = LONG_MAX;
+        rows = 256;
         for (int nj = 2; nj <= 4; ++nj) {
             const long tiles = (long)((V + 255) / 256) * ((N + 64 * nj - 1) / (64 * nj));
-            const long c = ((tiles + 255) / 256) * (2 * nj + 1);
+            const long c = ((tiles + 255) / 256) * (2 * nj + 5);
             if (c < cost) {
                 cost = c;
-                best = Shape{2, nj, 1};
+                best = Shape{2 + nj, 1};
+                states = 64 * nj;
             }
         }
     }
-    const long tiles = (long)((V + 128 * best.wv - 1) / (128 * best.wv)) * ((N + 64 * best.nj - 1) / (64 * best.nj));
+    const long tiles = (long)((V + rows - 1) / rows) * ((N + states - 1) / states);
     while (best.parts < 8 && tiles * best.parts * 2 <= 256 && blocks >= best.parts * 2 * 4) best.parts *= 2;
     return best;
 }
@@ -491,22 +483,11 @@ hipError_t launch_few(const MatmulF8Params &p, int parts, hipStream_t s) {
     }
 }
 
-template <typename T, int WV, int NJ>
+template <typename T, int K>
 hipError_t launch_tile(const MatmulF8Params &p, int parts, hipStream_t s) {
-    using S = Tile<WV, NJ>;
-    const auto kern = matmul_f8_kernel<T, WV, NJ>;
+    using S = typename TileOf<K>::type;
+    const auto kern = matmul_f8_kernel<T, S>;
     const int lds = S::buffers * S::buffer;
-    (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    const dim3 grid((p.V + S::rows - 1) / S::rows, (p.N + S::states - 1) / S::states, parts);
-    hipLaunchKernelGGL(kern, grid, dim3(S::threads), lds, s, p);
-    return hipGetLastError();
-}
-
-template <typename T, int NJ>
-hipError_t launch_turns(const MatmulF8Params &p, int parts, hipStream_t s) {
-    using S = Tile<2, NJ>;
-    const auto kern = matmul_f8_turns_kernel<T, NJ>;
-    const int lds = 2 * S::buffer;
     (void)hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     const dim3 grid((p.V + S::rows - 1) / S::rows, (p.N + S::states - 1) / S::states, parts);
     hipLaunchKernelGGL(kern, grid, dim3(S::threads), lds, s, p);
@@ -516,18 +497,18 @@ hipError_t launch_turns(const MatmulF8Params &p, int parts, hipStream_t s) {
 template <typename T>
 hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s) {
     hipError_t e;
-    switch (sh.wv * 10 + sh.nj) {
-        case 0: e = launch_few<T>(p, sh.parts, s); break;
-        case 11: e = launch_tile<T, 1, 1>(p, sh.parts, s); break;
-        case 12: e = launch_tile<T, 1, 2>(p, sh.parts, s); break;
-        case 13: e = launch_tile<T, 1, 3>(p, sh.parts, s); break;
-        case 14: e = launch_tile<T, 1, 4>(p, sh.parts, s); break;
-        case 22: e = launch_tile<T, 2, 2>(p, sh.parts, s); break;
-        case 32: e = launch_turns<T, 2>(p, sh.parts, s); break;
-        case 23: e = launch_tile<T, 2, 3>(p, sh.parts, s); break;
-        case 33: e = launch_turns<T, 3>(p, sh.parts, s); break;
-        case 24: e = launch_tile<T, 2, 4>(p, sh.parts, s); break;
-        case 34: e = launch_turns<T, 4>(p, sh.parts, s); break;
+    switch (sh.tile) {
+        case -1: e = launch_few<T>(p, sh.parts, s); break;
+        case 0: e = launch_tile<T, 0>(p, sh.parts, s); break;
+        case 1: e = launch_tile<T, 1>(p, sh.parts, s); break;
+        case 2: e = launch_tile<T, 2>(p, sh.parts, s); break;
+        case 3: e = launch_tile<T, 3>(p, sh.parts, s); break;
+        case 4: e = launch_tile<T, 4>(p, sh.parts, s); break;
+        case 5: e = launch_tile<T, 5>(p, sh.parts, s); break;
+        case 6: e = launch_tile<T, 6>(p, sh.parts, s); break;
+        case 7: e = launch_tile<T, 7>(p, sh.parts, s); break;
+        case 8: e = launch_tile<T, 8>(p, sh.parts, s); break;
+        case 9: e = launch_tile<T, 9>(p, sh.parts, s); break;
         default: return hipErrorInvalidValue;
     }
     if (e != hipSuccess || sh.parts == 1) return e;
