@@ -1,7 +1,6 @@
 // Matrix product in 8-bit floating point (e4m3) with a scale for each block of 128:
 //     out[n][v] = sum over b of xs[n][b] * ws[v / 128][b] * (sum over i in block b of x[n][i] * w[v][i]).
-#include <limits.h>
-
+#include <algorithm>
 #include <type_traits>
 
 #include "../../include/specee.h"
@@ -90,14 +89,16 @@ __device__ __forceinline__ void meet() {
 }
 
 // A workgroup's tile: WV by WN wavefronts, each with I * 16 rows of w by J * 16 of x
-template <int WV_, int WN_, int I_, int J_>
+// ONCE: no other workgroup reads its rows of w
+template <int WV_, int WN_, int I_, int J_, int BUFFERS, bool ONCE>
 struct Tile {
     static constexpr int WV = WV_, WN = WN_, I = I_, J = J_;
+    static constexpr bool once = ONCE;
     static constexpr int waves = WV * WN, threads = waves * kWave;
     static constexpr int rows = WV * I * 16, states = WN * J * 16;
     static constexpr int w_bytes = rows * kBlock, x_bytes = states * kBlock, groups = (states + 63) / 64;
     static constexpr int buffer = w_bytes + x_bytes + groups * 256;  // of one block, with the scales of x
-    static constexpr int buffers = 3 * buffer <= 156 * 1024 ? 3 : 2;
+    static constexpr int buffers = BUFFERS;
     static constexpr int w_loads = rows / 8 / waves, x_loads = states / 8 / waves;  // of a wavefront, 8 rows each
     static constexpr int loads = w_loads + x_loads + 1;
     static_assert(w_loads * waves * 8 == rows && x_loads * waves * 8 == states && 128 % (I * 16) == 0, "");
@@ -112,11 +113,10 @@ struct Loader {
     uint32_t woff[S::w_loads], xoff[S::x_loads], soff;
     uint32_t lds0;
     int d, piece, wave, lane;
-    bool once;  // whether this workgroup alone reads these rows of w
     unsigned char *smem;
 
     __device__ __forceinline__ Loader(const MatmulF8Params &p, int v0, int n0, int wave_, int lane_, unsigned char *smem_)
-        : d(p.d), wave(wave_), lane(lane_), once(gridDim.y == 1), smem(smem_) {
+        : d(p.d), wave(wave_), lane(lane_), smem(smem_) {
         lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) void *)smem;
         const int sub = lane >> 3;
         piece = ((lane & 7) ^ sub) * 16;
@@ -154,7 +154,7 @@ struct Loader {
 #pragma unroll
         for (int i = 0; i < S::w_loads; ++i) {
             const uint32_t to = lds0 + slot * S::buffer + (wave * S::w_loads + i) * 1024;
-            if (once)
+            if (S::once)
                 load_lds16_once(to, woff[i], wbase + k0);
             else
                 load_lds16(to, woff[i], wbase + k0);
@@ -220,19 +220,24 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
     const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
     const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
     const Loader<S> load(p, v0, n0, wave, lane, f8_smem);
+    // Rows of w that no other workgroup reads: the workgroups begin at different elements and go round, since rows a power of
+    // two apart have the same elements in few memory channels (60 states on 128256 x 8192, fp16 result: 226 -> 202 us).
+    // A result depends on its row of w alone, whatever N.
+    const int turn = S::once ? (int)(blockIdx.x * 37u % (unsigned)(b1 - b0)) : 0;
+    auto block = [&](int b) { return S::once && b + turn >= b1 ? b + turn - (b1 - b0) : b + turn; };
 
     floatx4 acc[I][J] = {};
     const int frag = c * kBlock + ((q ^ (c & 7)) << 4);
     const scalar_ptr ws = row_scales(p, v0 + wv * I * 16);
-    float sw = ws[b0];
+    float sw = ws[block(b0)];
     constexpr bool kTwo = S::buffers == 2;
 #pragma unroll
     for (int k = 0; k < S::buffers - 1; ++k)
         if (b0 + k < b1) {
-            load.load_x(b0 + k, k);
-            load.load_w(b0 + k, k);
+            load.load_x(block(b0 + k), k);
+            load.load_w(block(b0 + k), k);
         }
-    if (kTwo && b0 + 1 < b1) load.load_x(b0 + 1, 1);
+    if (kTwo && b0 + 1 < b1) load.load_x(block(b0 + 1), 1);
     for (int b = b0; b < b1; ++b) {
         const int slot = (b - b0) % S::buffers;
         if (b + 1 >= b1)
@@ -254,9 +259,9 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
                 xc[j] = read_codes(xt, j, frag);
                 s[j] = st[j * 16];
             }
-            if (b + 1 < b1) load.load_w(b + 1, slot ^ 1);
+            if (b + 1 < b1) load.load_w(block(b + 1), slot ^ 1);
             meet();
-            if (b + 2 < b1) load.load_x(b + 2, slot);
+            if (b + 2 < b1) load.load_x(block(b + 2), slot);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 x[j] = Operand(xc[j]);
@@ -265,8 +270,8 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
         } else {
             const int ahead = b + S::buffers - 1;
             if (ahead < b1) {
-                load.load_x(ahead, (ahead - b0) % S::buffers);
-                load.load_w(ahead, (ahead - b0) % S::buffers);
+                load.load_x(block(ahead), (ahead - b0) % S::buffers);
+                load.load_w(block(ahead), (ahead - b0) % S::buffers);
             }
 #pragma unroll
             for (int j = 0; j < J; ++j) {
@@ -274,7 +279,7 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
                 s[j] = st[j * 16] * sw;
             }
         }
-        const float sw_next = ws[min(b + 1, b1 - 1)];
+        const float sw_next = ws[block(min(b + 1, b1 - 1))];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             const Operand w(read_codes(wt, i, frag));
@@ -413,44 +418,46 @@ __global__ __launch_bounds__(1024) void matmul_f8_stream_kernel(MatmulF8Params p
     }
 }
 
-// The tiles that there are, by their number in kTiles
+// The tiles that there are, rows of w by rows of x.  Up to 128 rows of x are one tile wide, and w a stream; 128 x 128 fits
+// twice on a CU, where the one workgroup multiplies while the other waits; larger tiles read less per product.
 template <int K>
 struct TileOf;
-template <> struct TileOf<0> { using type = Tile<4, 1, 2, 2>; };
-template <> struct TileOf<1> { using type = Tile<4, 1, 2, 4>; };
-template <> struct TileOf<2> { using type = Tile<2, 2, 4, 4>; };
-template <> struct TileOf<3> { using type = Tile<1, 4, 8, 4>; };
-template <> struct TileOf<4> { using type = Tile<2, 4, 8, 2>; };
-template <> struct TileOf<5> { using type = Tile<2, 4, 8, 3>; };
-template <> struct TileOf<6> { using type = Tile<2, 4, 8, 4>; };
-template <> struct TileOf<7> { using type = Tile<2, 2, 4, 6>; };
-template <> struct TileOf<8> { using type = Tile<2, 2, 4, 2>; };
-template <> struct TileOf<9> { using type = Tile<4, 2, 4, 4>; };
+template <> struct TileOf<0> { using type = Tile<4, 1, 2, 2, 3, true>; };   // 128 x 32
+template <> struct TileOf<1> { using type = Tile<4, 1, 2, 4, 3, true>; };   // 128 x 64
+template <> struct TileOf<2> { using type = Tile<2, 2, 4, 4, 2, true>; };   // 128 x 128
+template <> struct TileOf<3> { using type = Tile<2, 2, 4, 4, 2, false>; };  // 128 x 128
+template <> struct TileOf<4> { using type = Tile<2, 4, 8, 3, 2, false>; };  // 256 x 192
+template <> struct TileOf<5> { using type = Tile<2, 4, 8, 4, 2, false>; };  // 256 x 256
 
 struct Shape {
     int tile, parts;  // tile -1: the stream for few states
 };
 
-Shape shape_of(int N, int V, int d) {
+Shape shape_of(int N, int V, int d, bool half) {
     const int blocks = (d + kBlock - 1) / kBlock;
     if (N <= 16) return Shape{-1, (blocks + kStreamBlocks - 1) / kStreamBlocks};
-    Shape best{N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 2 : 3, 1};
-    int rows = 128, states = N <= 32 ? 32 : N <= 64 ? 64 : N <= 128 ? 128 : 256;
-    if (N > 256) {
-        long cost = LONG_MAX;
-        rows = 256;
-        for (int nj = 2; nj <= 4; ++nj) {
-            const long tiles = (long)((V + 255) / 256) * ((N + 64 * nj - 1) / (64 * nj));
-            const long c = ((tiles + 255) / 256) * (2 * nj + 5);
+    auto tiles = [&](int rows, int states) { return (long)((V + rows - 1) / rows) * ((N + states - 1) / states); };
+    Shape best{N <= 32 ? 0 : N <= 64 ? 1 : 2, 1};
+    long n = tiles(128, 128);
+    if (N > 128) {
+        // What a block of 128 elements takes a CU, in 10 ns, measured at 8192 x 8192 x 8192: two workgroups of 128 x 128
+        // (one alone, at 512 x 5120 x 5120), one of 256 x 192, one of 256 x 256; the fp16 result, the fp32 result
+        const int both = half ? 125 : 195, alone = half ? 85 : 130, wide[2] = {half ? 170 : 260, half ? 208 : 370};
+        const long rest = n % 512;
+        long cost = n / 512 * both + (rest == 0 ? 0 : rest <= 256 ? alone : both);
+        best = Shape{3, 1};
+        for (int k = 0; k < 2; ++k) {
+            const long t = tiles(256, 192 + 64 * k), c = (t + 255) / 256 * wide[k];
             if (c < cost) {
                 cost = c;
-                best = Shape{2 + nj, 1};
-                states = 64 * nj;
+                best = Shape{4 + k, 1};
+                n = t;
             }
         }
     }
-    const long tiles = (long)((V + rows - 1) / rows) * ((N + states - 1) / states);
-    while (best.parts < 8 && tiles * best.parts * 2 <= 256 && blocks >= best.parts * 2 * 4) best.parts *= 2;
+    // parts of the elements while there is a CU for each and they are long enough (300 x 1024 x 5120: 32 us in one part,
+    // 17.5 in four, 18.7 in eight)
+    while (best.parts < 8 && n * best.parts * 2 <= 256 && blocks >= best.parts * 2 * 5) best.parts *= 2;
     return best;
 }
 
@@ -504,12 +511,7 @@ hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s)
         case 2: e = launch_tile<T, 2>(p, sh.parts, s); break;
         case 3: e = launch_tile<T, 3>(p, sh.parts, s); break;
         case 4: e = launch_tile<T, 4>(p, sh.parts, s); break;
-        case 5: e = launch_tile<T, 5>(p, sh.parts, s); break;
-        case 6: e = launch_tile<T, 6>(p, sh.parts, s); break;
-        case 7: e = launch_tile<T, 7>(p, sh.parts, s); break;
-        case 8: e = launch_tile<T, 8>(p, sh.parts, s); break;
-        case 9: e = launch_tile<T, 9>(p, sh.parts, s); break;
-        default: return hipErrorInvalidValue;
+        default: e = launch_tile<T, 5>(p, sh.parts, s); break;
     }
     if (e != hipSuccess || sh.parts == 1) return e;
     const size_t n = (size_t)p.N * p.V;
@@ -520,14 +522,15 @@ hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s)
 
 }  // namespace
 
+// (for either type of the result)
 size_t matmul_f8_workspace(int N, int V, int d) {
     if (N < 1) return 0;
-    const Shape s = shape_of(N, V, d);
-    return s.parts > 1 ? (size_t)s.parts * N * V * sizeof(float) : 0;
+    const int parts = std::max(shape_of(N, V, d, false).parts, shape_of(N, V, d, true).parts);
+    return parts > 1 ? (size_t)parts * N * V * sizeof(float) : 0;
 }
 
 hipError_t launch_matmul_f8(const MatmulF8Params &p, bool half, hipStream_t s) {
-    const Shape sh = shape_of(p.N, p.V, p.d);
+    const Shape sh = shape_of(p.N, p.V, p.d, half);
     return half ? launch_shape<half_t>(p, sh, s) : launch_shape<float>(p, sh, s);
 }
 
