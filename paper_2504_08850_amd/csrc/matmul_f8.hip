@@ -240,12 +240,12 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
     if (kTwo && b0 + 1 < b1) load.load_x(block(b0 + 1), 1);
     for (int b = b0; b < b1; ++b) {
         const int slot = (b - b0) % S::buffers;
-        if (b + 1 >= b1)
+        if (b + (kTwo ? 1 : S::buffers - 2) >= b1)
             landed<0>();
         else if (kTwo)
             landed<S::x_loads + 1>();  // the next block's x may be on its way
         else
-            landed<S::loads>();
+            landed<(S::buffers - 2) * S::loads>();
         const unsigned char *buf = f8_smem + slot * S::buffer;
         const unsigned char *wt = buf + wv * I * 16 * kBlock, *xt = buf + S::w_bytes + wn * J * 16 * kBlock;
         const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * J * 16 + c;
@@ -435,7 +435,9 @@ struct Shape {
 
 Shape shape_of(int N, int V, int d, bool half) {
     const int blocks = (d + kBlock - 1) / kBlock;
-    if (N <= 16) return Shape{-1, (blocks + kStreamBlocks - 1) / kStreamBlocks};
+    // few rows of w: the stream, whose workgroups cut the elements up and need no second launch to join them (one state, 1024 x
+    // 5120 6.9 us against 10.9 in tiles, 5120 x 5120 10.9 / 12.5; 8192 x 8192 20.6 / 18.5, 32000 x 4096 26.3 / 24.3)
+    if (N <= 16 && V <= 6144) return Shape{-1, (blocks + kStreamBlocks - 1) / kStreamBlocks};
     auto tiles = [&](int rows, int states) { return (long)((V + rows - 1) / rows) * ((N + states - 1) / states); };
     Shape best{N <= 32 ? 0 : N <= 64 ? 1 : 2, 1};
     long n = tiles(128, 128);
