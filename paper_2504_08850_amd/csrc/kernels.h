@@ -257,6 +257,7 @@ struct LogprobsGradParams {
     const int32_t *ids;
     const float *max_logit, *log_sum, *entropy, *g_logprobs, *g_entropy;
     void *grad;
+    bool once;  // set by the launcher: gradients too large for any cache
 };
 int logprobs_parts(int N, int V, bool half);
 hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s);
