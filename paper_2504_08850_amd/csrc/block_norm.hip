@@ -46,7 +46,7 @@ __device__ __forceinline__ void store_half8(half_t *p, const float *v) {
     __builtin_nontemporal_store(o, reinterpret_cast<half8 *>(p));
 }
 
-// EACH: every row has a gate of its own.  Otherwise branch_scale * gate * gamma_post is one factor per element, formed once.
+// EACH: every row has a gate of its own.  Otherwise gate * gamma_post, exact in fp32, is one factor per element, formed once.
 template <int VPT, bool EACH>
 __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormParams p) {
     __shared__ float part[2][2][16];
@@ -70,7 +70,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormParams p) {
         const half8 gate = load_half8((!EACH && p.gate ? p.gate : p.hidden) + at[j]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            factor[j][e] = p.gamma_post ? p.branch_scale * (float)post[e] : p.branch_scale;
+            factor[j][e] = p.gamma_post ? (float)post[e] : 1.f;
             if (!EACH && p.gate) factor[j][e] *= (float)gate[e];
         }
     }
@@ -85,7 +85,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormParams p) {
             hn[j] = load_half8_stream(p.hidden + next + at[j]);
             if (!p.branch) y[j] = zero_half8();
         }
-        float r_branch = 1.f;
+        float r_branch = p.branch_scale;
         if (p.gamma_post) {
             float ssq = 0.f;
 #pragma unroll
@@ -95,7 +95,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormParams p) {
                 for (int e = 0; e < 8; ++e) sum = fmaf((float)y[j][e], (float)y[j][e], sum);
                 ssq += in[j] ? sum : 0.f;
             }
-            r_branch = rsqrtf(workgroup_sum(ssq, part[turn][0]) / p.d + p.eps);
+            r_branch *= rsqrtf(workgroup_sum(ssq, part[turn][0]) / p.d + p.eps);
         }
         float s[VPT][8], ssq = 0.f;
 #pragma unroll
@@ -103,8 +103,7 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(BlockNormParams p) {
             float sum = 0.f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                float f = r_branch * factor[j][e];
-                if (EACH) f *= (float)g[j][e];
+                const float f = r_branch * (EACH ? factor[j][e] * (float)g[j][e] : factor[j][e]);
                 s[j][e] = fmaf((float)y[j][e], f, p.hidden_scale * (float)h[j][e]);
                 sum = fmaf(s[j][e], s[j][e], sum);
             }
