@@ -4,18 +4,22 @@
 //     dx_v = sum of g_t over ids t equal to v - p_v * (sum of g_t + g_H * (log p_v + H)).
 // m and log S are kept apart: their sum, the usual normaliser, would round away 1e-6 of every probability.
 //
-// Forward: one pass over the logits.  A lane keeps a reference r (an element of its own, at most 8 below its maximum), the
-// sums of exp(x - r) and exp(x - r)(x - r), and its largest element; 16 bytes are loaded per lane and step, rows may start at
-// any element (what lies before the first and behind the last whole 16 bytes is done one element per lane).  A logit of -inf
-// adds nothing (its t is cut at -300, and 2^-300 is 0 in fp32); NaN and +inf make the sum NaN, which is
-// looked at once at the end.
-// Alternatives cost the pass only the lanes' maxima.  At its end the lanes are folded to 64 groups, whose n-th largest
-// maximum tau is at most the n-th largest logit: only the few lanes that hold something of at least tau read their own
-// elements again, and sorted lists of 64 per wavefront, one entry per lane, take in what passes.  The order is by logit and
-// then by id, so the result does not depend on which wavefront saw what.
-// Few rows are cut into parts, one workgroup each, which a second launch joins.
+// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 322 us, 6.5 TB/s)
+// and by launch and latency below (1 x 32000: 6.8 us).  A lane keeps a reference r (an element of its own, at most 8 below its
+// maximum) and the sums of exp(x - r) and exp(x - r)(x - r): a new maximum seldom costs it a rescaling.  16 bytes are loaded
+// per lane and step; rows may start at any element (what lies before the first and behind the last whole 16 bytes is done one
+// element per lane).  A logit of -inf adds nothing (its t is cut at -300, and 2^-300 is 0 in fp32); NaN and +inf make the sum
+// NaN, which is looked at once at the end.
+// fp16 rows are bound by the vector instructions instead (2043 x 32003, 131 MB: 28 us): 7 for each element.
+// Alternatives cost the pass three instructions per 16 bytes: a lane keeps its largest granule's place and the maximum of the
+// others.  Behind the pass groups of 16 lanes meet, and the n-th largest of their maxima, tau, is at most the n-th largest
+// logit: only what reaches tau is read again and taken into sorted lists of 64 per wavefront, one entry per lane.  The order
+// is by logit and then by id, so the result does not depend on which wavefront saw what.
+// A few long rows are cut into parts that registers hold, one workgroup each, which a second launch joins.
 #include <float.h>
 #include <limits.h>
+
+#include <algorithm>
 
 #include "../../include/specee.h"
 #include "device_utils.h"
@@ -26,7 +30,6 @@ namespace specee {
 namespace {
 
 constexpr int kT = 512;  // threads of a workgroup
-constexpr int kWaves = kT / kWave;
 constexpr int kUnroll = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
@@ -318,11 +321,11 @@ __device__ __forceinline__ float row16_max(float v) {
     return fmaxf(v, dpp_f32<kDppMirror>(v));
 }
 
-// A row (or part) that a workgroup holds in registers, U granules per lane: the maximum first, then the sums about it and the
+// A part of a row that a workgroup holds in registers, U granules per lane: the maximum first, then the sums about it and the
 // alternatives, all from the registers.
-template <typename E, int T, int U>
-__global__ __launch_bounds__(T, 8) void logprobs_held_kernel(LogprobsParams p) {
-    constexpr int G = Granule<E>::n, WAVES = T / kWave, GROUPS = T / 16;
+template <typename E, int U>
+__global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) {
+    constexpr int T = kT, G = Granule<E>::n, WAVES = T / kWave, GROUPS = T / 16;
     const int n = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
@@ -390,15 +393,15 @@ __global__ __launch_bounds__(T, 8) void logprobs_held_kernel(LogprobsParams p) {
 
 // A row of any length, in steps.  A lane keeps the place of its largest granule and the maximum of the others: behind the pass
 // the lanes whose largest reaches tau read that granule again, and the few of which another does, all of theirs.
-template <typename E>
-__global__ __launch_bounds__(kT) void logprobs_kernel(LogprobsParams p) {
-    constexpr int G = Granule<E>::n, GROUPS = kT / 16;
+template <typename E, int T>
+__global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
+    constexpr int G = Granule<E>::n, GROUPS = T / 16, WAVES = T / kWave;
     const int n = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
     const E *body = row.p + row.head, *end = row.p + p.V - row.tail;
     __shared__ float groups[GROUPS], tau;
-    __shared__ RowEnd<kWaves> last;
+    __shared__ RowEnd<WAVES> last;
 
     LaneSum<E> a(LaneSum<E>::kLowest);
     float best = -INFINITY, others = -INFINITY;
@@ -413,24 +416,24 @@ __global__ __launch_bounds__(kT) void logprobs_kernel(LogprobsParams p) {
         best = fmaxf(best, c);
     };
     int g = tid;
-    for (; g - tid + kUnroll * kT <= row.whole; g += kUnroll * kT) {
+    for (; g - tid + kUnroll * T <= row.whole; g += kUnroll * T) {
         Granule<E> x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)(g + u * kT) * G);
+        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)(g + u * T) * G);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) take(x[u], g + u * kT);
+        for (int u = 0; u < kUnroll; ++u) take(x[u], g + u * T);
     }
     // The rest: at once in short rows, where its loads one after the other would take as long as all before (2043 x 32003 fp16
     // 34.5 -> 31 us); one by one in long ones, where other rows fill that time (4096 x 128256 fp32 327 us, at once 337)
-    if (row.whole > 32 * kT) {
-        for (; g < row.whole; g += kT) take(load_granule(body + (size_t)g * G), g);
+    if (row.whole > 32 * T) {
+        for (; g < row.whole; g += T) take(load_granule(body + (size_t)g * G), g);
     } else if (g - tid < row.whole) {
         Granule<E> x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)min(g + u * kT, row.whole - 1) * G);
+        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)min(g + u * T, row.whole - 1) * G);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
-            if (g + u * kT < row.whole) take(x[u], g + u * kT);
+            if (g + u * T < row.whole) take(x[u], g + u * T);
     }
     const bool extra = tid < row.head + row.tail;
     float xe = -INFINITY;
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(kT) void logprobs_kernel(LogprobsParams p) {
     __syncthreads();
     c = lane < GROUPS ? groups[lane] : -INFINITY;
     const float M = wave_max(c);
-    if (p.K) kth_largest<GROUPS, kWaves>(c, p.K, &tau);
+    if (p.K) kth_largest<GROUPS, WAVES>(c, p.K, &tau);
     a.move(M);
     TopList top;
     if (p.K) {
@@ -459,12 +462,12 @@ __global__ __launch_bounds__(kT) void logprobs_kernel(LogprobsParams p) {
             top.scan<G>(x.v, best, row.index(place), !several, least, p.K);
         }
         unsigned long long who = __ballot(several);
-        const int steps = (row.whole + kT - 1) / kT;
+        const int steps = (row.whole + T - 1) / T;
         while (who) {
             const int l = __ffsll(who) - 1;
             who &= who - 1;
             for (int i0 = 0; i0 < steps; i0 += kWave) {
-                const int gi = (i0 + lane) * kT + (tid - lane) + l;
+                const int gi = (i0 + lane) * T + (tid - lane) + l;
                 const bool has = gi < row.whole;
                 const Granule<E> x = load_granule(body + (size_t)(has ? gi : 0) * G);
                 top.scan<G>(x.v, largest(x), row.index(gi), has, least, p.K);
@@ -618,47 +621,39 @@ __global__ __launch_bounds__(kT) void logprobs_grad_kernel(LogprobsGradParams p)
 
 }  // namespace
 
-// How rows are dealt out.  A workgroup of 512 or 1024 threads holds up to 8 granules per thread, 64 or 128 KB of logits: rows
-// that fit are held, which reads them once and looks at the alternatives in registers.  Longer rows are cut into parts that
-// fit as long as there are few of them (the parts of a row are joined by a second launch), and read in steps where there
-// are enough rows for the GPU without.
+// How rows are dealt out: one workgroup per row, of 1024 threads where no CU has two rows and a row is long enough to give each
+// thread two steps (1 x 32000 fp32 with five alternatives 6.8 us, of 512 threads 7.8; 256 x 32000 10.0 and 10.8), else of 512
+// (511 x 32000 15.0 us, of 1024 threads 15.5; 2043 x 8000 18.7 and 26.2; 1 x 8000 4.7 and 4.8).  A few rows of more than 224 KB
+// in parts of at most 64 KB (fp16: 32 KB), which workgroups of 512 threads hold and a second launch joins (1 x 128256 fp32
+// 10.1 us, in one workgroup 14.3; 64 x 128256 14.8 and 16.3; but 100 x 128256 21 and 17, 1 x 50280 9.4 and 8.2).
 namespace {
 struct Deal {
-    int parts, threads, granules;  // granules per thread; 0: in steps
+    int parts, threads, granules;  // granules per thread that are held; 0: in steps
 };
 Deal deal(int N, int V, bool half) {
-    const int whole = V / (half ? 8 : 4) + 1;
-    Deal d{1, 512, 0};
-    if (whole > 8 * 1024) {
-        if (N >= 512) return d;
-        d.parts = (whole + 8 * 512 - 1) / (8 * 512);
-        const int more = 512 / (N > 0 ? N : 1);
-        if (more > d.parts) d.parts = more;
-        if (d.parts > kMaxParts) d.parts = kMaxParts;
+    const int whole = V / (half ? 8 : 4), most = (half ? 4 : 8) * kT;  // (8 of fp16 leave the registers)
+    if (N > 0 && N <= 64 && whole > 14336 && whole <= kMaxParts * (most - 1)) {
+        int parts = std::min(512 / N, kMaxParts);
+        while ((whole + parts - 1) / parts + 1 > most) ++parts;
+        return Deal{parts, kT, (whole + parts - 1) / parts + 1 <= 4 * kT ? 4 : 8};
     }
-    const int share = (whole + d.parts - 1) / d.parts + 1;
-    if (N >= 512) return Deal{1, 512, 0};
-    d.threads = share > 4 * 512 && share <= 8 * 1024 && (share > 8 * 512 || N < 128) ? 1024 : 512;
-    d.granules = (share + d.threads - 1) / d.threads;
-    if (d.granules > 8) return Deal{1, 512, 0};  // (a row that sixteen parts do not hold)
-    return d;
+    return Deal{1, N <= 256 && whole > 2048 ? 1024 : kT, 0};
 }
 template <typename E>
 hipError_t launch_rows(const LogprobsParams &p, const Deal &d, hipStream_t s) {
     const dim3 grid((unsigned)p.N * p.parts), threads(d.threads);
-    if (d.granules == 0)
-        hipLaunchKernelGGL(logprobs_kernel<E>, grid, threads, 0, s, p);
-    else if (d.threads == 1024 && d.granules <= 4)
-        hipLaunchKernelGGL((logprobs_held_kernel<E, 1024, 4>), grid, threads, 0, s, p);
-    else if (d.threads == 1024)
-        hipLaunchKernelGGL((logprobs_held_kernel<E, 1024, 8>), grid, threads, 0, s, p);
-    else if (d.granules <= 2)
-        hipLaunchKernelGGL((logprobs_held_kernel<E, 512, 2>), grid, threads, 0, s, p);
-    else if (d.granules <= 4)
-        hipLaunchKernelGGL((logprobs_held_kernel<E, 512, 4>), grid, threads, 0, s, p);
-    else
-        hipLaunchKernelGGL((logprobs_held_kernel<E, 512, 8>), grid, threads, 0, s, p);
-    if (p.parts > 1) hipLaunchKernelGGL(logprobs_join_kernel<E>, dim3(p.N), dim3(kJoinWaves * kWave), 0, s, p);
+    if (d.granules == 0) {
+        if (d.threads == 1024)
+            hipLaunchKernelGGL((logprobs_kernel<E, 1024>), grid, threads, 0, s, p);
+        else
+            hipLaunchKernelGGL((logprobs_kernel<E, kT>), grid, threads, 0, s, p);
+        return hipGetLastError();
+    }
+    if constexpr (sizeof(E) == 4) {
+        if (d.granules == 8) hipLaunchKernelGGL((logprobs_held_kernel<E, 8>), grid, threads, 0, s, p);
+    }
+    if (d.granules == 4) hipLaunchKernelGGL((logprobs_held_kernel<E, 4>), grid, threads, 0, s, p);
+    hipLaunchKernelGGL(logprobs_join_kernel<E>, dim3(p.N), dim3(kJoinWaves * kWave), 0, s, p);
     return hipGetLastError();
 }
 }  // namespace

@@ -226,9 +226,9 @@ size_t specee_workspace_bytes(int op, const specee_dims *dm, int n, int Mcap) {
                                                 : 0));
         case SPECEE_OP_MATMUL_F8:
             return check_f8(dm, n) ? (size_t)-1 : matmul_f8_workspace(n, dm->V, dm->d);
-        case SPECEE_OP_LOGPROBS:  // (fp16 rows are cut into no more parts than fp32 rows)
+        case SPECEE_OP_LOGPROBS:
             if (!dm || dm->V < 1 || n > 65535 || Mcap < 0 || Mcap > SPECEE_TOP_MAX) return (size_t)-1;
-            return logprobs_layout(n, logprobs_parts(n, dm->V, false), Mcap).total;
+            return logprobs_layout(n, std::max(logprobs_parts(n, dm->V, false), logprobs_parts(n, dm->V, true)), Mcap).total;
         case SPECEE_OP_LAYER_LOOP:
             if (check_dims(dm, true) || n > kLoopMaxTokens) return (size_t)-1;
             return loop_layout(n).total;

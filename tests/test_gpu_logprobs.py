@@ -101,7 +101,8 @@ def tokens(N, V, T, seed):
 @pytest.mark.parametrize("N,V,T,n_top", [(1, 1, 1, 1), (2, 2, 3, 5), (3, 7, 1, 32), (5, 50, 4, 20), (1, 777, 16, 8),
                                          (60, 777, 64, 32), (1, 32000, 1, 5), (2, 32003, 4, 20), (7, 24001, 0, 1),
                                          (513, 4099, 2, 3), (33, 50280, 1, 0), (1, 128256, 8, 32), (9, 128255, 8, 8),
-                                         (256, 2049, 1, 16), (300, 4097, 1, 31)])
+                                         (256, 2049, 1, 16), (300, 4097, 1, 31), (511, 9001, 1, 5), (64, 60001, 2, 9),
+                                         (3, 300007, 2, 32), (1, 262080, 1, 20)])
 def test_against_64_bits(sp, N, V, T, n_top, dtype):
     x = logits(N, V, dtype, N + V)
     ids = tokens(N, V, T, 3) if T else None
@@ -132,7 +133,7 @@ ROWS = {
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
-@pytest.mark.parametrize("N,V", [(1, 8200), (2, 33), (3, 32003), (600, 1030)])
+@pytest.mark.parametrize("N,V", [(1, 8200), (2, 33), (3, 32003), (600, 1030), (2, 128257)])
 @pytest.mark.parametrize("what", sorted(ROWS))
 def test_rows_that_are_special(sp, what, N, V, dtype):
     x = logits(N, V, dtype, 17)
@@ -147,7 +148,7 @@ def test_rows_that_are_special(sp, what, N, V, dtype):
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 @pytest.mark.parametrize("offset,pad", [(1, 0), (3, 5), (0, 7), (7, 64), (5, 1)])
 def test_rows_apart_and_off_any_alignment(sp, offset, pad, dtype):
-    for N, V in ((4, 301), (3, 16411), (1, 16411)):
+    for N, V in ((4, 301), (3, 16411), (1, 16411), (2, 110011)):
         buf = torch.full((offset + N * (V + pad),), 1000.0, dtype=dtype)   # what lies between would win
         x = buf[offset:].view(N, V + pad)[:, :V]
         x.copy_(logits(N, V, dtype, V + pad))
