@@ -418,16 +418,18 @@ __global__ __launch_bounds__(1024) void matmul_f8_stream_kernel(MatmulF8Params p
     }
 }
 
-// The tiles that there are, rows of w by rows of x.  Up to 128 rows of x are one tile wide, and w a stream; 128 x 128 fits
-// twice on a CU, where the one workgroup multiplies while the other waits; larger tiles read less per product.
+// The tiles that there are, rows of w by rows of x.  Up to 128 rows of x are one tile wide, and w a stream; up to 128 rows of w
+// fit twice on a CU, where the one workgroup multiplies while the other waits; larger tiles read less per product.
 template <int K>
 struct TileOf;
 template <> struct TileOf<0> { using type = Tile<4, 1, 2, 2, 3, true>; };   // 128 x 32
 template <> struct TileOf<1> { using type = Tile<4, 1, 2, 4, 3, true>; };   // 128 x 64
-template <> struct TileOf<2> { using type = Tile<2, 2, 4, 4, 2, true>; };   // 128 x 128
-template <> struct TileOf<3> { using type = Tile<2, 2, 4, 4, 2, false>; };  // 128 x 128
-template <> struct TileOf<4> { using type = Tile<2, 4, 8, 3, 2, false>; };  // 256 x 192
-template <> struct TileOf<5> { using type = Tile<2, 4, 8, 4, 2, false>; };  // 256 x 256
+template <> struct TileOf<2> { using type = Tile<4, 1, 4, 4, 3, true>; };   // 256 x 64
+template <> struct TileOf<3> { using type = Tile<2, 2, 4, 4, 2, true>; };   // 128 x 128
+template <> struct TileOf<4> { using type = Tile<4, 2, 4, 4, 2, true>; };   // 256 x 128, fp16 results
+template <> struct TileOf<5> { using type = Tile<2, 2, 4, 4, 2, false>; };  // 128 x 128
+template <> struct TileOf<6> { using type = Tile<2, 4, 8, 3, 2, false>; };  // 256 x 192
+template <> struct TileOf<7> { using type = Tile<2, 4, 8, 4, 2, false>; };  // 256 x 256
 
 struct Shape {
     int tile, parts;  // tile -1: the stream for few states
@@ -439,22 +441,30 @@ Shape shape_of(int N, int V, int d, bool half) {
     // 5120 6.9 us against 10.9 in tiles, 5120 x 5120 10.9 / 12.5; 8192 x 8192 20.6 / 18.5, 32000 x 4096 26.3 / 24.3)
     if (N <= 16 && V <= 6144) return Shape{-1, (blocks + kStreamBlocks - 1) / kStreamBlocks};
     auto tiles = [&](int rows, int states) { return (long)((V + rows - 1) / rows) * ((N + states - 1) / states); };
-    Shape best{N <= 32 ? 0 : N <= 64 ? 1 : 2, 1};
-    long n = tiles(128, 128);
-    if (N > 128) {
-        // What a block of 128 elements takes a CU, in 10 ns, measured at 8192 x 8192 x 8192: two workgroups of 128 x 128
-        // (one alone, at 512 x 5120 x 5120), one of 256 x 192, one of 256 x 256; the fp16 result, the fp32 result
-        const int both = half ? 125 : 195, alone = half ? 85 : 130, wide[2] = {half ? 170 : 260, half ? 208 : 370};
-        const long rest = n % 512;
-        long cost = n / 512 * both + (rest == 0 ? 0 : rest <= 256 ? alone : both);
-        best = Shape{3, 1};
-        for (int k = 0; k < 2; ++k) {
-            const long t = tiles(256, 192 + 64 * k), c = (t + 255) / 256 * wide[k];
-            if (c < cost) {
-                cost = c;
-                best = Shape{4 + k, 1};
-                n = t;
-            }
+    // What a block of 128 elements takes a CU, in 10 ns: two workgroups of a tile of 128 rows of w, one of them alone, one
+    // workgroup of larger tiles.  Measured with the fp16 result and with the fp32 result, for up to 64 rows of x and up to 128 on
+    // 65536 and 32768 x 4096 (below 64 rows, the 256 high tile: 50280 x 4096 51 -> 42 us, 128256 x 8192 203 -> 185 us; 32000 x
+    // 4096 27, in high tiles 39), for more at 8192 x 8192 x 8192 and 512 x 5120 x 5120.
+    struct Option {
+        int tile, rows, states, cost, alone;
+    };
+    static const Option options[2][8] = {
+        {{0, 128, 32, 1, 1}, {1, 128, 64, 182, 92}, {2, 256, 64, 152, 0}, {3, 128, 128, 216, 124}, {4, 256, 128, 200, 0},
+         {5, 128, 128, 125, 85}, {6, 256, 192, 170, 0}, {7, 256, 256, 208, 0}},
+        {{0, 128, 32, 1, 1}, {1, 128, 64, 192, 107}, {2, 256, 64, 177, 0}, {3, 128, 128, 265, 148}, {-1, 0, 0, 0, 0},
+         {5, 128, 128, 195, 130}, {6, 256, 192, 260, 0}, {7, 256, 256, 370, 0}}};
+    const int from = N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 3 : 5, to = N <= 32 ? 1 : N <= 64 ? 3 : N <= 128 ? 5 : 8;
+    Shape best{-1, 1};
+    long n = 0, least = 0;
+    for (int k = from; k < to; ++k) {
+        const Option &o = options[half ? 0 : 1][k];
+        if (o.rows == 0) continue;
+        const long t = tiles(o.rows, o.states), rest = t % 512;
+        const long cost = o.alone ? t / 512 * o.cost + (rest == 0 ? 0 : rest <= 256 ? o.alone : o.cost) : (t + 255) / 256 * o.cost;
+        if (best.tile < 0 || cost < least) {
+            least = cost;
+            best.tile = o.tile;
+            n = t;
         }
     }
     // parts of the elements while there is a CU for each and they are long enough (300 x 1024 x 5120: 32 us in one part,
@@ -512,8 +522,15 @@ hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s)
         case 1: e = launch_tile<T, 1>(p, sh.parts, s); break;
         case 2: e = launch_tile<T, 2>(p, sh.parts, s); break;
         case 3: e = launch_tile<T, 3>(p, sh.parts, s); break;
-        case 4: e = launch_tile<T, 4>(p, sh.parts, s); break;
-        default: e = launch_tile<T, 5>(p, sh.parts, s); break;
+        case 4:
+            if constexpr (sizeof(T) == 2)
+                e = launch_tile<T, 4>(p, sh.parts, s);
+            else
+                e = hipErrorInvalidValue;  // (not among this type's)
+            break;
+        case 5: e = launch_tile<T, 5>(p, sh.parts, s); break;
+        case 6: e = launch_tile<T, 6>(p, sh.parts, s); break;
+        default: e = launch_tile<T, 7>(p, sh.parts, s); break;
     }
     if (e != hipSuccess || sh.parts == 1) return e;
     const size_t n = (size_t)p.N * p.V;

@@ -66,7 +66,8 @@ def check(out, t, want=None):
 SHAPES = [(1, 1, 16), (1, 128, 128), (2, 129, 144), (1, 1000, 4096), (3, 300, 32), (5, 3, 1040), (16, 515, 1024), (17, 127, 112),
           (31, 257, 2048), (33, 777, 528), (60, 1000, 640), (64, 128, 256), (65, 130, 272), (127, 1, 128), (128, 128, 128),
           (129, 129, 129 * 16), (200, 650, 400), (257, 513, 384), (300, 1025, 1536), (520, 260, 144), (1, 40, 16384),
-          (20, 33, 28672), (4, 4099, 512), (1, 20011, 4112), (700, 1, 16), (1024, 1024, 1024)]
+          (20, 33, 28672), (4, 4099, 512), (1, 20011, 4112), (700, 1, 16), (1024, 1024, 1024),
+          (33, 33024, 272), (60, 50281, 400), (64, 33001, 1040), (100, 40003, 272), (128, 33030, 528)]
 
 
 @gpu
@@ -92,7 +93,8 @@ def test_every_code(sp, N, V, d):
 
 
 @gpu
-@pytest.mark.parametrize("N,V,d", [(1, 257, 272), (16, 130, 400), (70, 300, 144), (257, 257, 272)])
+@pytest.mark.parametrize("N,V,d", [(1, 257, 272), (16, 130, 400), (70, 300, 144), (257, 257, 272), (50, 33010, 400),
+                                   (100, 33010, 400)])
 def test_each_scale_reaches_its_own_block(sp, N, V, d):
     """One code of 1 per row of x, all weights 1: every output is one product of two scales, exactly."""
     nb, nv = (d + 127) // 128, (V + 127) // 128
