@@ -231,6 +231,9 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
     const scalar_ptr ws = row_scales(p, v0 + wv * I * 16);
     float sw = ws[block(b0)];
     constexpr bool kTwo = S::buffers == 2;
+    // Operands of w that are read together with x, before the workgroup meets (2043 x 5120 x 5120, fp16 result: 76 us with none,
+    // 68 with four; fp32 results, whose operands take twice the registers, gain nothing: 300 x 32000 x 4096 103 and 105)
+    constexpr int kEarly = sizeof(T) == 4 ? 0 : I < 4 ? I : 4;
 #pragma unroll
     for (int k = 0; k < S::buffers - 1; ++k)
         if (b0 + k < b1) {
@@ -251,38 +254,36 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
         const float *st = reinterpret_cast<const float *>(buf + S::w_bytes + S::x_bytes) + wn * J * 16 + c;
         float s[J];
         Operand x[J];
+        Codes xc[J], wc[I];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            xc[j] = read_codes(xt, j, frag);
+            s[j] = st[j * 16];
+        }
+#pragma unroll
+        for (int i = 0; i < kEarly; ++i) wc[i] = read_codes(wt, i, frag);
         if (kTwo) {
             // x is in registers once all have read it: its place is free for the block after the next
-            Codes xc[J];
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                xc[j] = read_codes(xt, j, frag);
-                s[j] = st[j * 16];
-            }
             if (b + 1 < b1) load.load_w(block(b + 1), slot ^ 1);
             meet();
             if (b + 2 < b1) load.load_x(block(b + 2), slot);
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                x[j] = Operand(xc[j]);
-                s[j] *= sw;
-            }
         } else {
             const int ahead = b + S::buffers - 1;
             if (ahead < b1) {
                 load.load_x(block(ahead), (ahead - b0) % S::buffers);
                 load.load_w(block(ahead), (ahead - b0) % S::buffers);
             }
+        }
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                x[j] = Operand(read_codes(xt, j, frag));
-                s[j] = st[j * 16] * sw;
-            }
+        for (int j = 0; j < J; ++j) {
+            x[j] = Operand(xc[j]);
+            s[j] *= sw;
         }
         const float sw_next = ws[block(min(b + 1, b1 - 1))];
 #pragma unroll
         for (int i = 0; i < I; ++i) {
-            const Operand w(read_codes(wt, i, frag));
+            if (i + kEarly < I) wc[i + kEarly] = read_codes(wt, i + kEarly, frag);
+            const Operand w(wc[i]);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
                 const floatx4 t = block_product(w, x[j]);
@@ -450,7 +451,7 @@ Shape shape_of(int N, int V, int d, bool half) {
     };
     static const Option options[2][8] = {
         {{0, 128, 32, 1, 1}, {1, 128, 64, 182, 92}, {2, 256, 64, 152, 0}, {3, 128, 128, 216, 124}, {4, 256, 128, 200, 0},
-         {5, 128, 128, 125, 85}, {6, 256, 192, 170, 0}, {7, 256, 256, 208, 0}},
+         {5, 128, 128, 123, 75}, {6, 256, 192, 155, 0}, {7, 256, 256, 207, 0}},
         {{0, 128, 32, 1, 1}, {1, 128, 64, 192, 107}, {2, 256, 64, 177, 0}, {3, 128, 128, 265, 148}, {-1, 0, 0, 0, 0},
          {5, 128, 128, 195, 130}, {6, 256, 192, 260, 0}, {7, 256, 256, 370, 0}}};
     const int from = N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 3 : 5, to = N <= 32 ? 1 : N <= 64 ? 3 : N <= 128 ? 5 : 8;
