@@ -10,7 +10,9 @@
 // per lane and step; rows may start at any element (what lies before the first and behind the last whole 16 bytes is done one
 // element per lane).  A logit of -inf adds nothing (its t is cut at -300, and 2^-300 is 0 in fp32); NaN and +inf make the sum
 // NaN, which is looked at once at the end.
-// fp16 rows are bound by the vector instructions instead (2043 x 32003, 131 MB: 28 us): 7 for each element.
+// Rows of 64 KB (2043 x 32003 fp16: 28 us, 4.8 TB/s; 27 without alternatives) are bound by what each does one after the other,
+// loads, meetings and second reads, with four rows on a CU: neither twice the loads in flight nor a fifth fewer vector
+// instructions (62 % of their time is used) made a difference.
 // Alternatives cost the pass three instructions per 16 bytes: a lane keeps its largest granule's place and the maximum of the
 // others.  Behind the pass groups of 16 lanes meet, and the n-th largest of their maxima, tau, is at most the n-th largest
 // logit: only what reaches tau is read again and taken into sorted lists of 64 per wavefront, one entry per lane.  The order
