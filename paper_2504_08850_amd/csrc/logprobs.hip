@@ -251,34 +251,84 @@ __device__ __forceinline__ void rank_entries(const float *v, const int *id, int 
     }
 }
 
-// What a workgroup's wavefronts leave for its end: their sums, and the entries of their lists in any order
+// What a workgroup's wavefronts leave for its end: their sums, and candidates for the alternatives in any order
 template <int WAVES>
 struct RowEnd {
+    static constexpr int kMost = WAVES * SPECEE_TOP_MAX;
     float s[WAVES], st[WAVES];
-    int entries;
-    float v[WAVES * SPECEE_TOP_MAX];
-    int id[WAVES * SPECEE_TOP_MAX];
+    int entries;  // 0 at a meeting of the workgroup before the first candidate; more than kMost: some had no place
+    float v[kMost];
+    int id[kMost];
 
-    // Behind a meeting of the workgroup that follows entries = 0
-    __device__ __forceinline__ void leave(float sum, float sumt, const TopList &top, int K) {
-        const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+    __device__ __forceinline__ void sums(float sum, float sumt) {
         sum = wave_sum(sum);
         sumt = wave_sum(sumt);
-        if (lane == 0) {
-            s[wave] = sum;
-            st[wave] = sumt;
+        if ((threadIdx.x & (kWave - 1)) == 0) {
+            s[threadIdx.x / kWave] = sum;
+            st[threadIdx.x / kWave] = sumt;
         }
+    }
+    // Places for c entries of a wavefront
+    __device__ __forceinline__ int places(int c) {
+        int first = 0;
+        if ((threadIdx.x & (kWave - 1)) == 0) first = atomicAdd(&entries, c);
+        return __builtin_amdgcn_readfirstlane(first);
+    }
+    // Whatever reaches tau; arguments as for TopList
+    template <int n, typename E>
+    __device__ __forceinline__ void scan(const E *x, float c, int at, bool has, float tau, int) {
+        const int lane = threadIdx.x & (kWave - 1);
+        const bool any = has && c >= tau && c > -INFINITY;
+        if (!__ballot(any)) return;
+        unsigned long long who[n];
+        int c_all = 0;
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+            who[j] = __ballot(any && (float)x[j] >= tau && (float)x[j] > -INFINITY);
+            c_all += __popcll(who[j]);
+        }
+        int first = places(c_all);
+#pragma unroll
+        for (int j = 0; j < n; ++j) {
+            const int k = first + __popcll(who[j] & ((1ull << lane) - 1));
+            if ((who[j] >> lane & 1) && k < kMost) {
+                v[k] = (float)x[j];
+                id[k] = at + j;
+            }
+            first += __popcll(who[j]);
+        }
+    }
+    __device__ __forceinline__ void leave(const TopList &top, int K) {
+        const int lane = threadIdx.x & (kWave - 1);
         const bool mine = lane < K && top.v > -INFINITY;
         const int c = __popcll(__ballot(mine));
-        int first = 0;
-        if (lane == 0 && c) first = atomicAdd(&entries, c);
-        first = __builtin_amdgcn_readfirstlane(first);
+        const int first = c ? places(c) : 0;
         if (mine) {
             v[first + lane] = top.v;
             id[first + lane] = top.id;
         }
     }
-    // Behind another: the row's or the part's outputs.  An entry's place is its rank: every lane holds one (or more), every
+    // The workgroup's candidates; each(to, tau) shows a wavefront's to to.scan().  MANY: all that reach tau, where they have a
+    // place (they nearly always do: without equal logits K alternatives have about K to 1.5 K of them); else each wavefront's
+    // best.  Follows and ends with a meeting.
+    template <bool MANY, typename F>
+    __device__ __forceinline__ void gather(float tau, int K, float sum, float sumt, const F &each) {
+        if (MANY) sums(sum, sumt);
+        if (MANY) {
+            each(*this, tau);
+            __syncthreads();
+            if (entries <= kMost) return;
+            __syncthreads();
+            if (threadIdx.x == 0) entries = 0;
+            __syncthreads();
+        }
+        TopList top;
+        each(top, tau);
+        if (!MANY) sums(sum, sumt);
+        leave(top, K);
+        __syncthreads();
+    }
+    // Behind a meeting: the row's or the part's outputs.  An entry's place is its rank: every lane holds one (or more), every
     // wavefront ranks its share of them.
     template <typename E>
     __device__ __forceinline__ void write(const LogprobsParams &p, int n, int part, const E *row, float M) const {
@@ -316,25 +366,32 @@ struct RowEnd {
     }
 };
 
-__device__ __forceinline__ float row16_max(float v) {
-    v = fmaxf(v, dpp_f32<kDppXor1>(v));
-    v = fmaxf(v, dpp_f32<kDppXor2>(v));
-    v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
-    return fmaxf(v, dpp_f32<kDppMirror>(v));
-}
+// Groups of 16 lanes, or 64 in all for many alternatives, whose tau comes the closer to the last of them
+template <int T, bool MANY>
+struct Groups {
+    static constexpr int n = MANY ? kWave : T / 16, lanes = T / n;
+    static_assert(lanes == 8 || lanes == 16, "");
+    __device__ static __forceinline__ float max(float v) {
+        v = fmaxf(v, dpp_f32<kDppXor1>(v));
+        v = fmaxf(v, dpp_f32<kDppXor2>(v));
+        v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+        return lanes == 8 ? v : fmaxf(v, dpp_f32<kDppMirror>(v));
+    }
+};
 
 // A part of a row that a workgroup holds in registers, U granules per lane: the maximum first, then the sums about it and the
 // alternatives, all from the registers.
-template <typename E, int U>
+template <typename E, int U, bool MANY>
 __global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) {
-    constexpr int T = kT, G = Granule<E>::n, WAVES = T / kWave, GROUPS = T / 16;
+    constexpr int T = kT, G = Granule<E>::n, WAVES = T / kWave;
     const int n = blockIdx.x / p.parts, part = blockIdx.x % p.parts;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
     const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
     const int g0 = (int)((long long)row.whole * part / p.parts), g1 = (int)((long long)row.whole * (part + 1) / p.parts);
     const int heads = part == 0 ? row.head : 0, tails = part == p.parts - 1 ? row.tail : 0;
     const E *body = row.p + row.head, *end = row.p + p.V - row.tail;
-    __shared__ float groups[GROUPS], tau;
+    using Group = Groups<T, MANY>;
+    __shared__ float groups[Group::n], tau;
     __shared__ RowEnd<WAVES> last;
 
     uintx4 raw[U];
@@ -359,11 +416,11 @@ __global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) 
         // (fp16 logits are widened again below: kept as floats they would cost half of the workgroups that a CU holds)
         if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
     }
-    c = row16_max(c);
-    if ((lane & 15) == 0) groups[tid / 16] = c;
+    c = Group::max(c);
+    if (tid % Group::lanes == 0) groups[tid / Group::lanes] = c;
     __syncthreads();
-    c = lane < GROUPS ? groups[lane] : -INFINITY;
-    if (p.K) kth_largest<GROUPS, WAVES>(c, p.K, &tau);
+    c = lane < Group::n ? groups[lane] : -INFINITY;
+    if (p.K) kth_largest<Group::n, WAVES>(c, p.K, &tau);
     const float M = wave_max(c);
     LaneSum<E> a(fmaxf(M, LaneSum<E>::kLowest));
 #pragma unroll
@@ -374,35 +431,37 @@ __global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) 
         if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
     }
     a.add(xe);
-    TopList top;
     if (p.K) {
         __syncthreads();
-        const float least = tau;
-        if (wave == 0 && heads) top.scan<1>(&xe, xe, lane, lane < heads, least, p.K);
+        last.template gather<MANY>(tau, p.K, a.s, a.st, [&](auto &to, float least) {
+            if (wave == 0 && heads) to.template scan<1>(&xe, xe, lane, lane < heads, least, p.K);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int g = g0 + u * T + tid;
-            const Granule<E> x = __builtin_bit_cast(Granule<E>, raw[u]);
-            top.scan<G>(x.v, largest(x), row.index(g), g < g1, least, p.K);
-        }
-        if (wave == 0 && tails)
-            top.scan<1>(&xe, xe, p.V - row.tail + lane - heads, lane >= heads && lane < heads + tails, least, p.K);
+            for (int u = 0; u < U; ++u) {
+                const int g = g0 + u * T + tid;
+                const Granule<E> x = __builtin_bit_cast(Granule<E>, raw[u]);
+                to.template scan<G>(x.v, largest(x), row.index(g), g < g1, least, p.K);
+            }
+            if (wave == 0 && tails)
+                to.template scan<1>(&xe, xe, p.V - row.tail + lane - heads, lane >= heads && lane < heads + tails, least, p.K);
+        });
+    } else {
+        last.sums(a.s, a.st);
+        __syncthreads();
     }
-    last.leave(a.s, a.st, top, p.K);
-    __syncthreads();
     last.write(p, n, part, row.p, M);
 }
 
 // A row of any length, in steps.  A lane keeps the place of its largest granule and the maximum of the others: behind the pass
 // the lanes whose largest reaches tau read that granule again, and the few of which another does, all of theirs.
-template <typename E, int T>
+template <typename E, int T, bool MANY>
 __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
-    constexpr int G = Granule<E>::n, GROUPS = T / 16, WAVES = T / kWave;
+    constexpr int G = Granule<E>::n, WAVES = T / kWave;
     const int n = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
     const E *body = row.p + row.head, *end = row.p + p.V - row.tail;
-    __shared__ float groups[GROUPS], tau;
+    using Group = Groups<T, MANY>;
+    __shared__ float groups[Group::n], tau;
     __shared__ RowEnd<WAVES> last;
 
     LaneSum<E> a(LaneSum<E>::kLowest);
@@ -445,55 +504,64 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
         a.add(xe);
     }
     if (tid == 0) last.entries = 0;
-    float c = row16_max(fmaxf(best, xe == xe ? xe : -INFINITY));
-    if ((lane & 15) == 0) groups[tid / 16] = c;
+    float c = Group::max(fmaxf(best, xe == xe ? xe : -INFINITY));
+    if (tid % Group::lanes == 0) groups[tid / Group::lanes] = c;
     __syncthreads();
-    c = lane < GROUPS ? groups[lane] : -INFINITY;
+    c = lane < Group::n ? groups[lane] : -INFINITY;
     const float M = wave_max(c);
-    if (p.K) kth_largest<GROUPS, WAVES>(c, p.K, &tau);
+    if (p.K) kth_largest<Group::n, WAVES>(c, p.K, &tau);
     a.move(M);
-    TopList top;
     if (p.K) {
         __syncthreads();
-        const float least = tau;
-        top.scan<1>(&xe, xe, tid < row.head ? tid : p.V - row.tail + tid - row.head, extra, least, p.K);
-        const bool several = others >= least && others > -INFINITY;
-        if (__ballot(best >= least && best > -INFINITY && !several)) {
-            Granule<E> x = {};
-            if (best >= least && !several && row.whole > 0) x = load_granule(body + (size_t)place * G);
-            top.scan<G>(x.v, best, row.index(place), !several, least, p.K);
-        }
-        unsigned long long who = __ballot(several);
-        const int steps = (row.whole + T - 1) / T;
-        while (who) {
-            const int l = __ffsll(who) - 1;
-            who &= who - 1;
-            for (int i0 = 0; i0 < steps; i0 += kWave) {
-                const int gi = (i0 + lane) * T + (tid - lane) + l;
-                const bool has = gi < row.whole;
-                const Granule<E> x = load_granule(body + (size_t)(has ? gi : 0) * G);
-                top.scan<G>(x.v, largest(x), row.index(gi), has, least, p.K);
+        last.template gather<MANY>(tau, p.K, a.s, a.st, [&](auto &to, float least) {
+            to.template scan<1>(&xe, xe, tid < row.head ? tid : p.V - row.tail + tid - row.head, extra, least, p.K);
+            const bool several = others >= least && others > -INFINITY;
+            if (__ballot(best >= least && best > -INFINITY && !several)) {
+                Granule<E> x = {};
+                if (best >= least && !several && row.whole > 0) x = load_granule(body + (size_t)place * G);
+                to.template scan<G>(x.v, best, row.index(place), !several, least, p.K);
             }
-        }
+            unsigned long long who = __ballot(several);
+            const int steps = (row.whole + T - 1) / T;
+            while (who) {
+                const int l = __ffsll(who) - 1;
+                who &= who - 1;
+                for (int i0 = 0; i0 < steps; i0 += kWave) {
+                    const int gi = (i0 + lane) * T + (tid - lane) + l;
+                    const bool has = gi < row.whole;
+                    const Granule<E> x = load_granule(body + (size_t)(has ? gi : 0) * G);
+                    to.template scan<G>(x.v, largest(x), row.index(gi), has, least, p.K);
+                }
+            }
+        });
+    } else {
+        last.sums(a.s, a.st);
+        __syncthreads();
     }
-    last.leave(a.s, a.st, top, p.K);
-    __syncthreads();
     last.write(p, n, 0, row.p, M);
 }
 
-// Joins the parts of a row
-constexpr int kJoinWaves = 8;
+// Joins the parts of a row.  A thread holds one of their candidates, as an integer of the same order (by logit, where the two
+// zeros are one, and then by id), and counts those above it among a share of all; the wavefronts that would hold none take
+// further shares.
+constexpr int kJoinT = kMaxParts * SPECEE_TOP_MAX, kJoinWaves = kJoinT / kWave;
 template <typename E>
-__global__ __launch_bounds__(kJoinWaves * kWave) void logprobs_join_kernel(LogprobsParams p) {
+__global__ __launch_bounds__(kJoinT) void logprobs_join_kernel(LogprobsParams p) {
     const int n = blockIdx.x, tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
     const E *row = static_cast<const E *>(p.logits) + (long long)n * p.stride;
-    __shared__ float v[kMaxParts * SPECEE_TOP_MAX];
-    __shared__ int id[kMaxParts * SPECEE_TOP_MAX];
-    const int C = p.parts * p.K;  // (at most one entry per thread; places without one hold -inf and INT_MAX)
+    __shared__ unsigned long long keys[kJoinT];
+    __shared__ int above[kJoinT], real;
+    const int C = p.parts * p.K;
+    float x = -INFINITY;  // (places without a candidate hold -inf)
+    int id = INT_MAX;
     if (tid < C) {
-        v[tid] = p.part_vals[(size_t)n * C + tid];
-        id[tid] = p.part_ids[(size_t)n * C + tid];
+        x = p.part_vals[(size_t)n * C + tid];
+        id = p.part_ids[(size_t)n * C + tid];
+        keys[tid] = (unsigned long long)ordered(x + 0.f) << 32 | (uint32_t)~id;
+        above[tid] = 0;
     }
+    if (tid == 0) real = 0;
     float r = -INFINITY;
     LaneSum<E> a(0.f);
     if (lane < p.parts) {
@@ -510,12 +578,19 @@ __global__ __launch_bounds__(kJoinWaves * kWave) void logprobs_join_kernel(Logpr
     write_tokens(p, n, row, st, tid);
     if (p.K == 0) return;
     __syncthreads();
-    int real = 0;
-    for (int o = 0; o < C; o += kWave) real += __popcll(__ballot(o + lane < C && v[min(o + lane, C - 1)] > -INFINITY));
+    const int groups = (C + kWave - 1) / kWave, shares = kJoinWaves / groups, share = wave / groups;
+    const int mine = wave % groups * kWave + lane;
+    if (share < shares) {
+        const unsigned long long key = keys[min(mine, C - 1)];
+        int count = 0;
+        for (int e = share; e < C; e += shares) count += keys[e] > key;
+        if (mine < C && count) atomicAdd(&above[mine], count);
+    }
+    const int has = __popcll(__ballot(x > -INFINITY));
+    if (lane == 0 && has) atomicAdd(&real, has);
+    __syncthreads();
+    if (x > -INFINITY && above[tid] < p.K) write_alternative(p, n, above[tid], st, x, id);
     if (tid >= real && tid < p.K) write_alternative(p, n, tid, st, -INFINITY, INT_MAX);
-    rank_entries<kJoinWaves>(v, id, C, p.K, [&](int k, float x, int i) {
-        if (x > -INFINITY) write_alternative(p, n, k, st, x, i);
-    });
 }
 
 // Gradient: elementwise, one workgroup per kGradSteps * 512 granules of a row; the ids that fall into its share are looked
@@ -641,21 +716,24 @@ Deal deal(int N, int V, bool half) {
     }
     return Deal{1, N <= 256 && whole > 2048 ? 1024 : kT, 0};
 }
-template <typename E>
+// More than a few alternatives in kernels of their own (2043 x 8000 fp16, 20 alternatives: 22 us, in those for a few 26; five: 18
+// and 16.7)
+constexpr int kFew = 8;
+template <typename E, bool MANY>
 hipError_t launch_rows(const LogprobsParams &p, const Deal &d, hipStream_t s) {
     const dim3 grid((unsigned)p.N * p.parts), threads(d.threads);
     if (d.granules == 0) {
         if (d.threads == 1024)
-            hipLaunchKernelGGL((logprobs_kernel<E, 1024>), grid, threads, 0, s, p);
+            hipLaunchKernelGGL((logprobs_kernel<E, 1024, MANY>), grid, threads, 0, s, p);
         else
-            hipLaunchKernelGGL((logprobs_kernel<E, kT>), grid, threads, 0, s, p);
+            hipLaunchKernelGGL((logprobs_kernel<E, kT, MANY>), grid, threads, 0, s, p);
         return hipGetLastError();
     }
     if constexpr (sizeof(E) == 4) {
-        if (d.granules == 8) hipLaunchKernelGGL((logprobs_held_kernel<E, 8>), grid, threads, 0, s, p);
+        if (d.granules == 8) hipLaunchKernelGGL((logprobs_held_kernel<E, 8, MANY>), grid, threads, 0, s, p);
     }
-    if (d.granules == 4) hipLaunchKernelGGL((logprobs_held_kernel<E, 4>), grid, threads, 0, s, p);
-    hipLaunchKernelGGL(logprobs_join_kernel<E>, dim3(p.N), dim3(kJoinWaves * kWave), 0, s, p);
+    if (d.granules == 4) hipLaunchKernelGGL((logprobs_held_kernel<E, 4, MANY>), grid, threads, 0, s, p);
+    hipLaunchKernelGGL(logprobs_join_kernel<E>, dim3(p.N), dim3(kJoinT), 0, s, p);
     return hipGetLastError();
 }
 }  // namespace
@@ -666,7 +744,8 @@ int logprobs_parts(int N, int V, bool half) {
 
 hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s) {
     const Deal d = deal(p.N, p.V, half);
-    return half ? launch_rows<half_t>(p, d, s) : launch_rows<float>(p, d, s);
+    if (p.K > kFew) return half ? launch_rows<half_t, true>(p, d, s) : launch_rows<float, true>(p, d, s);
+    return half ? launch_rows<half_t, false>(p, d, s) : launch_rows<float, false>(p, d, s);
 }
 
 hipError_t launch_logprobs_grad(const LogprobsGradParams &params, bool half, hipStream_t s) {

@@ -146,6 +146,19 @@ def test_rows_that_are_special(sp, what, N, V, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("V", [6000, 20000, 128257])
+@pytest.mark.parametrize("n_top", [1, 32])
+def test_equal_logits_by_the_hundred(sp, n_top, V, dtype):
+    counts = (31, 33, 255, 256, 257, 511, 512, 513, 2000)
+    x = logits(len(counts), V, dtype, 23)
+    for n, c in enumerate(counts):
+        x[n, torch.randperm(V, generator=torch.Generator().manual_seed(c))[:c]] = 30.0
+    x[3:, 7] = 31.0                                # and one above them
+    check(sp.logprobs(x.cuda(), None, n_top=n_top), x, None, n_top)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 @pytest.mark.parametrize("offset,pad", [(1, 0), (3, 5), (0, 7), (7, 64), (5, 1)])
 def test_rows_apart_and_off_any_alignment(sp, offset, pad, dtype):
     for N, V in ((4, 301), (3, 16411), (1, 16411), (2, 110011)):
