@@ -439,11 +439,12 @@ struct TileOf;
 template <> struct TileOf<0> { using type = Tile<4, 1, 2, 2, 3, true>; };   // 128 x 32
 template <> struct TileOf<1> { using type = Tile<4, 1, 2, 4, 3, true>; };   // 128 x 64
 template <> struct TileOf<2> { using type = Tile<4, 1, 4, 4, 3, true>; };   // 256 x 64
-template <> struct TileOf<3> { using type = Tile<2, 2, 4, 4, 2, true>; };   // 128 x 128
-template <> struct TileOf<4> { using type = Tile<4, 2, 4, 4, 2, true>; };   // 256 x 128, fp16 results
-template <> struct TileOf<5> { using type = Tile<2, 2, 4, 4, 2, false>; };  // 128 x 128
-template <> struct TileOf<6> { using type = Tile<2, 4, 8, 3, 2, false>; };  // 256 x 192
-template <> struct TileOf<7> { using type = Tile<2, 4, 8, 4, 2, false>; };  // 256 x 256
+template <> struct TileOf<3> { using type = Tile<8, 1, 4, 4, 2, true>; };   // 512 x 64, fp16 results
+template <> struct TileOf<4> { using type = Tile<2, 2, 4, 4, 2, true>; };   // 128 x 128
+template <> struct TileOf<5> { using type = Tile<4, 2, 4, 4, 2, true>; };   // 256 x 128, fp16 results
+template <> struct TileOf<6> { using type = Tile<2, 2, 4, 4, 2, false>; };  // 128 x 128
+template <> struct TileOf<7> { using type = Tile<2, 4, 8, 3, 2, false>; };  // 256 x 192
+template <> struct TileOf<8> { using type = Tile<2, 4, 8, 4, 2, false>; };  // 256 x 256
 
 struct Shape {
     int tile, parts;  // tile -1: the stream for few states
@@ -457,17 +458,17 @@ Shape shape_of(int N, int V, int d, bool half) {
     auto tiles = [&](int rows, int states) { return (long)((V + rows - 1) / rows) * ((N + states - 1) / states); };
     // What a block of 128 elements takes a CU, in 10 ns: two workgroups of a tile of 128 rows of w, one of them alone, one
     // workgroup of larger tiles.  Measured with the fp16 result and with the fp32 result, for up to 64 rows of x and up to 128 on
-    // 65536 and 32768 x 4096 (below 64 rows, the 256 high tile: 50280 x 4096 51 -> 42 us, 128256 x 8192 203 -> 185 us; 32000 x
-    // 4096 27, in high tiles 39), for more at 8192 x 8192 x 8192 and 512 x 5120 x 5120.
+    // 131072, 65536 and 32768 x 4096 (60 rows, fp16: 50280 x 4096 51 -> 42 us in tiles of 256; 128256 x 8192 203 -> 187 in those
+    // and 172 in tiles of 512; 32000 x 4096 27, in tiles of 256 39), for more at 8192 x 8192 x 8192 and 512 x 5120 x 5120.
     struct Option {
         int tile, rows, states, cost, alone;
     };
-    static const Option options[2][8] = {
-        {{0, 128, 32, 1, 1}, {1, 128, 64, 182, 92}, {2, 256, 64, 152, 0}, {3, 128, 128, 216, 124}, {4, 256, 128, 200, 0},
-         {5, 128, 128, 123, 75}, {6, 256, 192, 155, 0}, {7, 256, 256, 207, 0}},
-        {{0, 128, 32, 1, 1}, {1, 128, 64, 192, 107}, {2, 256, 64, 177, 0}, {3, 128, 128, 265, 148}, {-1, 0, 0, 0, 0},
-         {5, 128, 128, 195, 130}, {6, 256, 192, 260, 0}, {7, 256, 256, 370, 0}}};
-    const int from = N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 3 : 5, to = N <= 32 ? 1 : N <= 64 ? 3 : N <= 128 ? 5 : 8;
+    static const Option options[2][9] = {
+        {{0, 128, 32, 1, 1}, {1, 128, 64, 182, 92}, {2, 256, 64, 152, 0}, {3, 512, 64, 282, 0}, {4, 128, 128, 216, 124},
+         {5, 256, 128, 200, 0}, {6, 128, 128, 123, 75}, {7, 256, 192, 155, 0}, {8, 256, 256, 207, 0}},
+        {{0, 128, 32, 1, 1}, {1, 128, 64, 192, 107}, {2, 256, 64, 177, 0}, {-1, 0, 0, 0, 0}, {4, 128, 128, 265, 148},
+         {-1, 0, 0, 0, 0}, {6, 128, 128, 195, 130}, {7, 256, 192, 260, 0}, {8, 256, 256, 370, 0}}};
+    const int from = N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 4 : 6, to = N <= 32 ? 1 : N <= 64 ? 4 : N <= 128 ? 6 : 9;
     Shape best{-1, 1};
     long n = 0, least = 0;
     for (int k = from; k < to; ++k) {
@@ -529,22 +530,20 @@ hipError_t launch_tile(const MatmulF8Params &p, int parts, hipStream_t s) {
 
 template <typename T>
 hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s) {
-    hipError_t e;
+    hipError_t e = hipErrorInvalidValue;
+    if constexpr (sizeof(T) == 2) {
+        if (sh.tile == 3) e = launch_tile<T, 3>(p, sh.parts, s);
+        if (sh.tile == 5) e = launch_tile<T, 5>(p, sh.parts, s);
+    }
     switch (sh.tile) {
         case -1: e = launch_few<T>(p, sh.parts, s); break;
         case 0: e = launch_tile<T, 0>(p, sh.parts, s); break;
         case 1: e = launch_tile<T, 1>(p, sh.parts, s); break;
         case 2: e = launch_tile<T, 2>(p, sh.parts, s); break;
-        case 3: e = launch_tile<T, 3>(p, sh.parts, s); break;
-        case 4:
-            if constexpr (sizeof(T) == 2)
-                e = launch_tile<T, 4>(p, sh.parts, s);
-            else
-                e = hipErrorInvalidValue;  // (not among this type's)
-            break;
-        case 5: e = launch_tile<T, 5>(p, sh.parts, s); break;
+        case 4: e = launch_tile<T, 4>(p, sh.parts, s); break;
         case 6: e = launch_tile<T, 6>(p, sh.parts, s); break;
-        default: e = launch_tile<T, 7>(p, sh.parts, s); break;
+        case 7: e = launch_tile<T, 7>(p, sh.parts, s); break;
+        case 8: e = launch_tile<T, 8>(p, sh.parts, s); break;
     }
     if (e != hipSuccess || sh.parts == 1) return e;
     const size_t n = (size_t)p.N * p.V;

@@ -67,7 +67,7 @@ SHAPES = [(1, 1, 16), (1, 128, 128), (2, 129, 144), (1, 1000, 4096), (3, 300, 32
           (31, 257, 2048), (33, 777, 528), (60, 1000, 640), (64, 128, 256), (65, 130, 272), (127, 1, 128), (128, 128, 128),
           (129, 129, 129 * 16), (200, 650, 400), (257, 513, 384), (300, 1025, 1536), (520, 260, 144), (1, 40, 16384),
           (20, 33, 28672), (4, 4099, 512), (1, 20011, 4112), (700, 1, 16), (1024, 1024, 1024),
-          (33, 33024, 272), (60, 50281, 400), (64, 33001, 1040), (100, 40003, 272), (128, 33030, 528)]
+          (33, 33024, 272), (60, 50281, 400), (40, 99000, 272), (64, 131072, 144), (50, 130050, 144), (64, 33001, 1040), (100, 40003, 272), (128, 33030, 528)]
 
 
 @gpu
