@@ -102,7 +102,7 @@ __device__ __forceinline__ void meet() {
 }
 
 // A workgroup's tile: WV by WN wavefronts, each with I * 16 rows of w by J * 16 of x
-// ONCE: no other workgroup reads its rows of w
+// ONCE: no other workgroup reads its rows of w (or w is small)
 template <int WV_, int WN_, int I_, int J_, int BUFFERS, bool ONCE>
 struct Tile {
     static constexpr int WV = WV_, WN = WN_, I = I_, J = J_;
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
     const int b0 = (int)((long long)p.blocks * blockIdx.z / gridDim.z);
     const int b1 = (int)((long long)p.blocks * (blockIdx.z + 1) / gridDim.z);
     const Loader<S> load(p, v0, n0, wave, lane, f8_smem);
-    // Rows of w that no other workgroup reads: the workgroups begin at different elements and go round, since rows a power of
+    // Rows of w that are read once: the workgroups begin at different elements and go round, since rows a power of
     // two apart have the same elements in few memory channels (60 states on 128256 x 8192, fp16 result: 226 -> 202 us).
     // A result depends on its row of w alone, whatever N.
     const int turn = S::once ? (int)(blockIdx.x * 37u % (unsigned)(b1 - b0)) : 0;
@@ -471,7 +471,17 @@ Shape shape_of(int N, int V, int d, bool half) {
     const int from = N <= 32 ? 0 : N <= 64 ? 1 : N <= 128 ? 4 : 6, to = N <= 32 ? 1 : N <= 64 ? 4 : N <= 128 ? 6 : 9;
     Shape best{-1, 1};
     long n = 0, least = 0;
-    for (int k = from; k < to; ++k) {
+    // Small matrices, which the caches hold: the smallest tiles that leave no CU with two (512 x 2048 x 2048, fp32 result: 21 us
+    // in tiles of 128 x 128, 12 of 128 x 32; 1000 x 1000 x 1024 12.9 and 7.5; 60 x 2048 x 2048 11.8 and 9.8 of 128 x 64 and 128 x
+    // 32, but 40 x 8192 x 8192 23 and 25)
+    if (N > 32 && (long)V * d <= 24l << 20)
+        for (int k = 1; k >= 0; --k)
+            if (tiles(128, 32 << k) <= 256) {
+                best.tile = k;
+                n = tiles(128, 32 << k);
+            }
+    const bool small = best.tile >= 0;
+    for (int k = from; k < to && !small; ++k) {
         const Option &o = options[half ? 0 : 1][k];
         if (o.rows == 0) continue;
         const long t = tiles(o.rows, o.states), rest = t % 512;
@@ -482,8 +492,8 @@ Shape shape_of(int N, int V, int d, bool half) {
             n = t;
         }
     }
-    // parts of the elements while there is a CU for each and they are long enough (300 x 1024 x 5120: 32 us in one part,
-    // 17.5 in four, 18.7 in eight)
+    // parts of the elements while there is a CU for each and they are long enough (40 x 8192 x 8192, fp32 result: 49 us in one
+    // part, 30 in two, 23 in four, 27 in eight)
     while (best.parts < 8 && n * best.parts * 2 <= 256 && blocks >= best.parts * 2 * 5) best.parts *= 2;
     return best;
 }

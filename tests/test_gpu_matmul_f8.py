@@ -67,7 +67,8 @@ SHAPES = [(1, 1, 16), (1, 128, 128), (2, 129, 144), (1, 1000, 4096), (3, 300, 32
           (31, 257, 2048), (33, 777, 528), (60, 1000, 640), (64, 128, 256), (65, 130, 272), (127, 1, 128), (128, 128, 128),
           (129, 129, 129 * 16), (200, 650, 400), (257, 513, 384), (300, 1025, 1536), (520, 260, 144), (1, 40, 16384),
           (20, 33, 28672), (4, 4099, 512), (1, 20011, 4112), (700, 1, 16), (1024, 1024, 1024),
-          (33, 33024, 272), (60, 50281, 400), (40, 99000, 272), (64, 131072, 144), (50, 130050, 144), (64, 33001, 1040), (100, 40003, 272), (128, 33030, 528)]
+          (33, 33024, 272), (60, 50281, 400), (40, 99000, 272), (64, 131072, 144), (50, 130050, 144), (64, 33001, 1040), (100, 40003, 272), (128, 33030, 528), (70, 31001, 144),
+          (2100, 1100, 272), (4200, 2100, 144), (4000, 3100, 272)]
 
 
 @gpu
@@ -94,7 +95,7 @@ def test_every_code(sp, N, V, d):
 
 @gpu
 @pytest.mark.parametrize("N,V,d", [(1, 257, 272), (16, 130, 400), (70, 300, 144), (257, 257, 272), (50, 33010, 400),
-                                   (100, 33010, 400)])
+                                   (100, 33010, 400), (2100, 1100, 272), (4000, 3100, 272)])
 def test_each_scale_reaches_its_own_block(sp, N, V, d):
     """One code of 1 per row of x, all weights 1: every output is one product of two scales, exactly."""
     nb, nv = (d + 127) // 128, (V + 127) // 128
@@ -125,7 +126,8 @@ def test_a_nan_reaches_its_row_or_column_alone_and_neighbours_are_left(sp, N):
 
 
 @gpu
-@pytest.mark.parametrize("N,V,d", [(1, 4096, 4096), (16, 1030, 2048), (60, 2100, 1040), (300, 300, 528)])
+@pytest.mark.parametrize("N,V,d", [(1, 4096, 4096), (16, 1030, 2048), (60, 2100, 1040), (300, 300, 528), (50, 33010, 400),
+                                   (2100, 1100, 528), (4000, 3100, 272)])
 def test_same_bits_graphs_and_streams(sp, N, V, d):
     t = up(inputs(N, V, d, 3))
     for dtype in (torch.float32, torch.float16):
