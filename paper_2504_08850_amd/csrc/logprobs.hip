@@ -231,22 +231,27 @@ struct TopList {
     }
 };
 
-// Calls put(rank, x, id) on one lane for each of the C entries (in LDS) whose rank is below K, by x and then by id
+// Calls put(rank, x, id) on one lane for each of the C entries (in LDS) whose rank is below K, by x and then by id.  Up to 64: an
+// entry per lane, and the wavefronts count for their share of them; more: a thread counts for its own.
 template <int WAVES, typename F>
 __device__ __forceinline__ void rank_entries(const float *v, const int *id, int C, int K, const F &put) {
-    const int lane = threadIdx.x & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    if (C > kWave) {
+        for (int e = tid; e < C; e += WAVES * kWave) {
+            const float x = v[e];
+            const int i = id[e];
+            int rank = 0;
+            for (int o = 0; o < C; ++o) rank += v[o] > x || (v[o] == x && id[o] < i);
+            if (rank < K) put(rank, x, i);
+        }
+        return;
+    }
     const float mv = lane < C ? v[lane] : -INFINITY;
     const int mi = lane < C ? id[lane] : INT_MAX;
     for (int e = wave; e < C; e += WAVES) {
         const float x = v[e];
         const int i = id[e];
-        int rank = __popcll(__ballot(mv > x || (mv == x && mi < i)));
-        for (int o = kWave; o < C; o += kWave) {
-            const bool has = o + lane < C;
-            const float ov = has ? v[o + lane] : -INFINITY;
-            const int oi = has ? id[o + lane] : INT_MAX;
-            rank += __popcll(__ballot(ov > x || (ov == x && oi < i)));
-        }
+        const int rank = __popcll(__ballot(mv > x || (mv == x && mi < i)));
         if (rank < K && lane == 0) put(rank, x, i);
     }
 }
@@ -254,7 +259,8 @@ __device__ __forceinline__ void rank_entries(const float *v, const int *id, int 
 // What a workgroup's wavefronts leave for its end: their sums, and candidates for the alternatives in any order
 template <int WAVES>
 struct RowEnd {
-    static constexpr int kMost = WAVES * SPECEE_TOP_MAX;
+    // (room for every wavefront's best, and for rows that have fewer granules than there are alternatives)
+    static constexpr int kMost = WAVES < 8 ? 8 * SPECEE_TOP_MAX : WAVES * SPECEE_TOP_MAX;
     float s[WAVES], st[WAVES];
     int entries;  // 0 at a meeting of the workgroup before the first candidate; more than kMost: some had no place
     float v[kMost];
@@ -366,16 +372,17 @@ struct RowEnd {
     }
 };
 
-// Groups of 16 lanes, or 64 in all for many alternatives, whose tau comes the closer to the last of them
+// Groups of 16 lanes, or 64 groups for many alternatives, whose tau comes the closer to the last of them
 template <int T, bool MANY>
 struct Groups {
     static constexpr int n = MANY ? kWave : T / 16, lanes = T / n;
-    static_assert(lanes == 8 || lanes == 16, "");
+    static_assert(lanes == 4 || lanes == 8 || lanes == 16, "");
     __device__ static __forceinline__ float max(float v) {
         v = fmaxf(v, dpp_f32<kDppXor1>(v));
         v = fmaxf(v, dpp_f32<kDppXor2>(v));
-        v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
-        return lanes == 8 ? v : fmaxf(v, dpp_f32<kDppMirror>(v));
+        if (lanes > 4) v = fmaxf(v, dpp_f32<kDppHalfMirror>(v));
+        if (lanes > 8) v = fmaxf(v, dpp_f32<kDppMirror>(v));
+        return v;
     }
 };
 
@@ -476,25 +483,28 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
         place = c > best ? g : place;
         best = fmaxf(best, c);
     };
-    int g = tid;
-    for (; g - tid + kUnroll * T <= row.whole; g += kUnroll * T) {
+    // Rows with less than a granule per lane: dealt out to the groups in turn, so that as many as can have one
+    const int lane0 = row.whole < T ? tid % Group::lanes * Group::n + tid / Group::lanes : tid;
+    int g0 = 0;
+    for (; g0 + kUnroll * T <= row.whole; g0 += kUnroll * T) {
         Granule<E> x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)(g + u * T) * G);
+        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)(g0 + u * T + lane0) * G);
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) take(x[u], g + u * T);
+        for (int u = 0; u < kUnroll; ++u) take(x[u], g0 + u * T + lane0);
     }
     // The rest: at once in short rows, where its loads one after the other would take as long as all before (2043 x 32003 fp16
     // 34.5 -> 31 us); one by one in long ones, where other rows fill that time (4096 x 128256 fp32 327 us, at once 337)
     if (row.whole > 32 * T) {
-        for (; g < row.whole; g += T) take(load_granule(body + (size_t)g * G), g);
-    } else if (g - tid < row.whole) {
+        for (int g = g0 + lane0; g < row.whole; g += T) take(load_granule(body + (size_t)g * G), g);
+    } else if (g0 < row.whole) {
         Granule<E> x[kUnroll];
 #pragma unroll
-        for (int u = 0; u < kUnroll; ++u) x[u] = load_granule_once(body + (size_t)min(g + u * T, row.whole - 1) * G);
+        for (int u = 0; u < kUnroll; ++u)
+            x[u] = load_granule_once(body + (size_t)min(g0 + u * T + lane0, row.whole - 1) * G);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u)
-            if (g + u * T < row.whole) take(x[u], g + u * T);
+            if (g0 + u * T + lane0 < row.whole) take(x[u], g0 + u * T + lane0);
     }
     const bool extra = tid < row.head + row.tail;
     float xe = -INFINITY;
@@ -593,7 +603,7 @@ __global__ __launch_bounds__(kJoinT) void logprobs_join_kernel(LogprobsParams p)
     if (tid >= real && tid < p.K) write_alternative(p, n, tid, st, -INFINITY, INT_MAX);
 }
 
-// Gradient: elementwise, one workgroup per kGradSteps * 512 granules of a row; the ids that fall into its share are looked
+// Gradient: elementwise, one workgroup per kGradSteps * T granules of a row; the ids that fall into its share are looked
 // for once and kept in LDS, in their order, so that ids that repeat add up the same way every time.
 constexpr int kGradSteps = 4;
 
@@ -605,13 +615,13 @@ struct GradRow {
     }
 };
 
-template <typename E>
-__global__ __launch_bounds__(kT) void logprobs_grad_kernel(LogprobsGradParams p) {
+template <typename E, int T>
+__global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) {
     constexpr int G = Granule<E>::n;
     const int n = blockIdx.y, tid = threadIdx.x, lane = tid & (kWave - 1);
     const RowView<E> row(static_cast<const E *>(p.logits) + (long long)n * p.stride, p.V);
     E *out = static_cast<E *>(p.grad) + (long long)n * p.grad_stride;
-    const int g0 = blockIdx.x * (kGradSteps * kT), g1 = min(row.whole, g0 + kGradSteps * kT);
+    const int g0 = blockIdx.x * (kGradSteps * T), g1 = min(row.whole, g0 + kGradSteps * T);
     const bool first = blockIdx.x == 0, last = blockIdx.x == gridDim.x - 1;
     const E *body = row.p + row.head;
     // elements of this workgroup
@@ -642,7 +652,7 @@ __global__ __launch_bounds__(kT) void logprobs_grad_kernel(LogprobsGradParams p)
     Granule<E> x[kGradSteps];
 #pragma unroll
     for (int u = 0; u < kGradSteps; ++u) {
-        const int g = g0 + u * kT + tid;
+        const int g = g0 + u * T + tid;
         if (g < g1) x[u] = load_granule_once(body + (size_t)g * G);
     }
     const int extras = (first ? row.head : 0) + (last ? row.tail : 0);
@@ -664,7 +674,7 @@ __global__ __launch_bounds__(kT) void logprobs_grad_kernel(LogprobsGradParams p)
     const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0;
 #pragma unroll
     for (int u = 0; u < kGradSteps; ++u) {
-        const int g = g0 + u * kT + tid;
+        const int g = g0 + u * T + tid;
         if (g < g1) {
             const int at = row.index(g);
             float d[G];
@@ -700,9 +710,10 @@ __global__ __launch_bounds__(kT) void logprobs_grad_kernel(LogprobsGradParams p)
 
 // How rows are dealt out: one workgroup per row, of 1024 threads where no CU has two rows and a row is long enough to give each
 // thread two steps (1 x 32000 fp32 with five alternatives 6.8 us, of 512 threads 7.8; 256 x 32000 10.0 and 10.8), else of 512
-// (511 x 32000 15.0 us, of 1024 threads 15.5; 2043 x 8000 18.7 and 26.2; 1 x 8000 4.7 and 4.8).  A few rows of more than 224 KB
-// in parts of at most 64 KB (fp16: 32 KB), which workgroups of 512 threads hold and a second launch joins (1 x 128256 fp32
-// 10.1 us, in one workgroup 14.3; 64 x 128256 14.8 and 16.3; but 100 x 128256 21 and 17, 1 x 50280 9.4 and 8.2).
+// (511 x 32000 15.0 us, of 1024 threads 15.5; 1 x 8000 4.7 and 4.8), and of 256 where there are many short ones (one alternative,
+// 3317 x 777 fp32 18 -> 11 us, 4096 x 8000 28 -> 26, fp16 25 -> 19; but 600 x 8000 8.5 and 8.8, 2043 x 32003 43 and 46).  A few
+// rows of more than 224 KB in parts of at most 64 KB (fp16: 32 KB), which workgroups of 512 threads hold and a second launch joins
+// (1 x 128256 fp32 10.1 us, in one workgroup 14.3; 64 x 128256 14.8 and 16.3; but 100 x 128256 21 and 17, 1 x 50280 9.4 and 8.2).
 namespace {
 struct Deal {
     int parts, threads, granules;  // granules per thread that are held; 0: in steps
@@ -714,7 +725,7 @@ Deal deal(int N, int V, bool half) {
         while ((whole + parts - 1) / parts + 1 > most) ++parts;
         return Deal{parts, kT, (whole + parts - 1) / parts + 1 <= 4 * kT ? 4 : 8};
     }
-    return Deal{1, N <= 256 && whole > 2048 ? 1024 : kT, 0};
+    return Deal{1, N <= 256 && whole > 2048 ? 1024 : N > 1024 && whole <= 2048 ? 256 : kT, 0};
 }
 // More than a few alternatives in kernels of their own (2043 x 8000 fp16, 20 alternatives: 22 us, in those for a few 26; five: 18
 // and 16.7)
@@ -725,6 +736,8 @@ hipError_t launch_rows(const LogprobsParams &p, const Deal &d, hipStream_t s) {
     if (d.granules == 0) {
         if (d.threads == 1024)
             hipLaunchKernelGGL((logprobs_kernel<E, 1024, MANY>), grid, threads, 0, s, p);
+        else if (d.threads == 256)
+            hipLaunchKernelGGL((logprobs_kernel<E, 256, MANY>), grid, threads, 0, s, p);
         else
             hipLaunchKernelGGL((logprobs_kernel<E, kT, MANY>), grid, threads, 0, s, p);
         return hipGetLastError();
@@ -748,18 +761,26 @@ hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s) {
     return half ? launch_rows<half_t, false>(p, d, s) : launch_rows<float, false>(p, d, s);
 }
 
+namespace {
+template <typename E, int T>
+hipError_t launch_grad(const LogprobsGradParams &p, int whole, hipStream_t s) {
+    const int share = kGradSteps * T;
+    hipLaunchKernelGGL((logprobs_grad_kernel<E, T>), dim3(whole < 1 ? 1 : (whole + share - 1) / share, p.N), dim3(T), 0, s, p);
+    return hipGetLastError();
+}
+}  // namespace
+
 hipError_t launch_logprobs_grad(const LogprobsGradParams &params, bool half, hipStream_t s) {
     // no cache keeps more than this from one pass to the next (4096 x 32000 fp16: 104 us without the hint, 94 with it;
     // 60 x 32003 fp32: 6.2 and 7.3)
     LogprobsGradParams p = params;
     p.once = (size_t)p.N * p.V * (half ? 2 : 4) > (64u << 20);
-    const int whole = p.V / (half ? 8 : 4), share = kGradSteps * kT;
-    const dim3 grid(whole < 1 ? 1 : (whole + share - 1) / share, p.N);
-    if (half)
-        hipLaunchKernelGGL(logprobs_grad_kernel<half_t>, grid, dim3(kT), 0, s, p);
-    else
-        hipLaunchKernelGGL(logprobs_grad_kernel<float>, grid, dim3(kT), 0, s, p);
-    return hipGetLastError();
+    // many short rows by two wavefronts each (4096 x 1030 fp32 13.9 -> 9.5 us, 4096 x 2000 fp16 15.6 -> 11.0; but 60 x 777 3.9 and
+    // 5.3)
+    const int whole = p.V / (half ? 8 : 4);
+    if (p.N > 512 && whole <= kGradSteps * 128)
+        return half ? launch_grad<half_t, 128>(p, whole, s) : launch_grad<float, 128>(p, whole, s);
+    return half ? launch_grad<half_t, kT>(p, whole, s) : launch_grad<float, kT>(p, whole, s);
 }
 
 }  // namespace specee
