@@ -374,8 +374,8 @@ int specee_block_norm(const specee_dims *dims, int N, const specee_half *hidden,
  *   x [N][d], x_scales [N][ceil(d/128)]; weight [V][d] (row v = output v), w_scales [ceil(V/128)][ceil(d/128)]; blocks at
  *   the end may be shorter.  out, out_f16 [N][V]: one of them, the other NULL.
  * Products and sums are fp32.  For an fp32 result they are formed from the codes as halves, exactly; for an fp16 result
- * from the codes on the 8-bit matrix cores, which line products of 128 elements up with the largest of them: off by 2e-5 to
- * 5e-5 of a sum, a twentieth or less of the rounding of the result.
+ * from the codes on the 8-bit matrix cores, which line products of 128 elements up with the largest of them: off by 1e-5 to
+ * 5e-5 of the 2-norm of a block's products (up to 4e-4 for single sums), where fp16 rounds by up to 5e-4.
  * d: a multiple of 16, at most 65536; only dims->d and dims->V are read.
  * Workspace: SPECEE_OP_MATMUL_F8 with n = N.
  */

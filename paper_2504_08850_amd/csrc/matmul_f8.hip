@@ -2,8 +2,8 @@
 //     out[n][v] = sum over b of xs[n][b] * ws[v / 128][b] * (sum over i in block b of x[n][i] * w[v][i]).
 // The sum of a block is one matrix instruction of 16 x 16 x 128 (or four of 32) into zeros; one multiply-add in fp32 folds it
 // into the result with the product of its scales, so every block is scaled once, exactly as it was quantised.
-// fp16 results take the codes as they are: the instruction aligns its 128 products before it adds them, which is off by up to
-// 5e-5 of the block's 2-norm, below a tenth of the result's own rounding.  fp32 results would show that: their codes become
+// fp16 results take the codes as they are: the instruction aligns its 128 products before it adds them, which is off by 1e-5 to
+// 5e-5 of their 2-norm, a tenth of what the result's own rounding is at that size.  fp32 results would show that: their codes become
 // halves first (exact) and are multiplied by the fp16 instruction (off by 1e-7), at twice the time per product.
 //
 // Few rows of x are a stream over w: 1 x 32000 x 4096 takes 23.5 us and 60 x 128256 x 8192 in fp32 198 us, 5.6 and 5.4 TB/s of w
