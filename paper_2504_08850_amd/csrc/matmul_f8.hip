@@ -244,9 +244,12 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
     const scalar_ptr ws = row_scales(p, v0 + wv * I * 16);
     float sw = ws[block(b0)];
     constexpr bool kTwo = S::buffers == 2;
-    // Operands of w that are read together with x, before the workgroup meets (2043 x 5120 x 5120, fp16 result: 76 us with none,
-    // 68 with four; fp32 results, whose operands take twice the registers, gain nothing: 300 x 32000 x 4096 103 and 105)
-    constexpr int kEarly = sizeof(T) == 4 ? 0 : I < 4 ? I : 4;
+    // Where x has one place less the workgroup meets once x is in registers.  Operands of w that are read together with it (512 x
+    // 5120 x 5120, fp16 result: 35 us with none, 30.5 with four; fp32 results, whose operands take twice the registers, gain
+    // nothing: 300 x 32000 x 4096 103 and 105), and the row of tiles before which the workgroup meets: wavefronts of eight
+    // rows begin to multiply before (8192 x 8192 x 8192 fp16 540 -> 528 us; those of four lose, 30.5 -> 33.5).
+    constexpr int kEarly = sizeof(T) == 4 ? 0 : I == 8 ? 2 : I < 4 ? I : 4;
+    constexpr int kMeet = sizeof(T) == 2 && I == 8 ? 2 : 0;
 #pragma unroll
     for (int k = 0; k < S::buffers - 1; ++k)
         if (b0 + k < b1) {
@@ -278,8 +281,10 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
         if (kTwo) {
             // x is in registers once all have read it: its place is free for the block after the next
             if (b + 1 < b1) load.load_w(block(b + 1), slot ^ 1);
-            meet();
-            if (b + 2 < b1) load.load_x(block(b + 2), slot);
+            if (kMeet == 0) {
+                meet();
+                if (b + 2 < b1) load.load_x(block(b + 2), slot);
+            }
         } else {
             const int ahead = b + S::buffers - 1;
             if (ahead < b1) {
@@ -296,6 +301,12 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
 #pragma unroll
         for (int i = 0; i < I; ++i) {
             if (i + kEarly < I) wc[i + kEarly] = read_codes(wt, i + kEarly, frag);
+            if (kTwo && kMeet > 0 && i == kMeet) {
+                __builtin_amdgcn_sched_barrier(0);
+                meet();
+                if (b + 2 < b1) load.load_x(block(b + 2), slot);
+                __builtin_amdgcn_sched_barrier(0);
+            }
             const Operand w(wc[i]);
 #pragma unroll
             for (int j = 0; j < J; ++j) {
