@@ -4,8 +4,8 @@
 //     dx_v = sum of g_t over ids t equal to v - p_v * (sum of g_t + g_H * (log p_v + H)).
 // m and log S are kept apart: their sum, the usual normaliser, would round away 1e-6 of every probability.
 //
-// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 322 us, 6.5 TB/s)
-// and by launch and latency below (1 x 32000: 6.8 us).  A lane keeps a reference r (an element of its own, at most 8 below its
+// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 319 us, 6.6
+// TB/s) and by launch and latency below (1 x 32000: 6.4 us).  A lane keeps a reference r (an element of its own, at most 8 below its
 // maximum) and the sums of exp(x - r) and exp(x - r)(x - r): a new maximum seldom costs it a rescaling.  16 bytes are loaded
 // per lane and step; rows may start at any element (what lies before the first and behind the last whole 16 bytes is done one
 // element per lane).  A logit of -inf adds nothing (its t is cut at -300, and 2^-300 is 0 in fp32); NaN and +inf make the sum
@@ -14,9 +14,10 @@
 // loads, meetings and second reads, with four rows on a CU: neither twice the loads in flight nor a fifth fewer vector
 // instructions (62 % of their time is used) made a difference.
 // Alternatives cost the pass three instructions per 16 bytes: a lane keeps its largest granule's place and the maximum of the
-// others.  Behind the pass groups of 16 lanes meet, and the n-th largest of their maxima, tau, is at most the n-th largest
-// logit: only what reaches tau is read again and taken into sorted lists of 64 per wavefront, one entry per lane.  The order
-// is by logit and then by id, so the result does not depend on which wavefront saw what.
+// others.  Behind the pass groups of lanes meet, and the n-th largest of their maxima, tau, is at most the n-th largest logit:
+// only what reaches tau is read again, and taken into a sorted list per wavefront, one entry per lane (a few alternatives), or
+// gathered and ranked as it is (many).  The order is by logit and then by id, so the result does not depend on which wavefront
+// saw what.
 // A few long rows are cut into parts that registers hold, one workgroup each, which a second launch joins.
 #include <float.h>
 #include <limits.h>
@@ -319,8 +320,8 @@ struct RowEnd {
     // best.  Follows and ends with a meeting.
     template <bool MANY, typename F>
     __device__ __forceinline__ void gather(float tau, int K, float sum, float sumt, const F &each) {
-        if (MANY) sums(sum, sumt);
         if (MANY) {
+            sums(sum, sumt);
             each(*this, tau);
             __syncthreads();
             if (entries <= kMost) return;
@@ -334,8 +335,7 @@ struct RowEnd {
         leave(top, K);
         __syncthreads();
     }
-    // Behind a meeting: the row's or the part's outputs.  An entry's place is its rank: every lane holds one (or more), every
-    // wavefront ranks its share of them.
+    // Behind a meeting: the row's or the part's outputs.  An entry's place is its rank.
     template <typename E>
     __device__ __forceinline__ void write(const LogprobsParams &p, int n, int part, const E *row, float M) const {
         const int tid = threadIdx.x;
