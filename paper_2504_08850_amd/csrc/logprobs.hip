@@ -242,6 +242,7 @@ __device__ __forceinline__ void rank_entries(const float *v, const int *id, int 
             const float x = v[e];
             const int i = id[e];
             int rank = 0;
+#pragma unroll 8
             for (int o = 0; o < C; ++o) rank += v[o] > x || (v[o] == x && id[o] < i);
             if (rank < K) put(rank, x, i);
         }
@@ -593,6 +594,7 @@ __global__ __launch_bounds__(kJoinT) void logprobs_join_kernel(LogprobsParams p)
     if (share < shares) {
         const unsigned long long key = keys[min(mine, C - 1)];
         int count = 0;
+#pragma unroll 8
         for (int e = share; e < C; e += shares) count += keys[e] > key;
         if (mine < C && count) atomicAdd(&above[mine], count);
     }
