@@ -2,17 +2,20 @@
 // the gradient of the first two.  With m = max x, S = sum exp(x - m):
 //     log p(v) = (x_v - m) - log S,   H = log S - sum exp(x - m) (x - m) / S,
 //     dx_v = sum of g_t over ids t equal to v - p_v * (sum of g_t + g_H * (log p_v + H)).
-// m and log S are kept apart: their sum, the usual normaliser, would round away 1e-6 of every probability.
+// m and log S are kept apart: their sum, the usual normaliser, would round away 1e-6 of every probability.  So are the 1 that m
+// itself is in S, and the rest u: where one token is all but certain, log S = log(1 + u) is about u, and S as one number would
+// hold u to 6e-8 of 1 instead of 6e-8 of itself.
 //
-// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 319 us, 6.6
-// TB/s) and by launch and latency below (1 x 32000: 6.4 us).  A lane keeps a reference r (an element of its own, at most 8 below its
-// maximum) and the sums of exp(x - r) and exp(x - r)(x - r): a new maximum seldom costs it a rescaling.  16 bytes are loaded
-// per lane and step; rows may start at any element (what lies before the first and behind the last whole 16 bytes is done one
-// element per lane).  A logit of -inf adds nothing (its t is cut at -300, and 2^-300 is 0 in fp32); NaN and +inf make the sum
-// NaN, which is looked at once at the end.
-// Rows of 64 KB (2043 x 32003 fp16: 28 us, 4.8 TB/s; 27 without alternatives) are bound by what each does one after the other,
-// loads, meetings and second reads, with four rows on a CU: neither twice the loads in flight nor a fifth fewer vector
-// instructions (62 % of their time is used) made a difference.
+// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 320 us, 6.6
+// TB/s) and by launch and latency below (1 x 32000: 6.7 us).  A lane keeps its largest element out of its sums, and of the others
+// the sums of exp(x - r) and exp(x - r)(x - r) about a reference r (an element of its own, at most 8 below its maximum): a new
+// maximum seldom costs it a rescaling.  The largest of 16 bytes and the rest come from minima and maxima in pairs, one
+// instruction per element (with S as one number: 1 x 32000 6.4 us, 64 x 128256 14.1 against 14.5, 2043 x 32003 fp16 27.6
+// against 28.6).  16 bytes are loaded per lane and step; rows may start at any element (what lies before the first and behind the
+// last whole 16 bytes is done one element per lane).  A logit of -inf adds nothing (its t is cut at -300, and 2^-300 is 0 in
+// fp32); NaN makes the sum NaN, +inf is the maximum: both are looked at once at the end.
+// Rows of 64 KB (2043 x 32003 fp16: 28.6 us, 4.6 TB/s) are bound by what each does one after the other, loads, meetings and
+// second reads, with four rows on a CU: neither twice the loads in flight nor a fifth fewer vector instructions made a difference.
 // Alternatives cost the pass three instructions per 16 bytes: a lane keeps its largest granule's place and the maximum of the
 // others.  Behind the pass groups of lanes meet, and the n-th largest of their maxima, tau, is at most the n-th largest logit:
 // only what reaches tau is read again, and taken into a sorted list per wavefront, one entry per lane (a few alternatives), or
@@ -23,6 +26,7 @@
 #include <limits.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/specee.h"
 #include "device_utils.h"
@@ -72,7 +76,7 @@ struct RowView {
 };
 
 // Sums about a reference r, in base 2: t = (x - r) log2 e.  fp16 logits form t in one mixed instruction from x and the rounded
-// product r log2 e (RowStats puts back what was rounded off); fp32 logits, which may be near the ends of their type, from x - r.
+// product r log2 e (about_exactly puts back what was rounded off); fp32 logits, which may be near the ends of their type, from x - r.
 template <typename E>
 struct LaneSum {
     static constexpr bool kMixed = sizeof(E) == 2;
@@ -88,8 +92,9 @@ struct LaneSum {
     }
     __device__ __forceinline__ explicit LaneSum(float ref) : s(0.f), st(0.f) { about(ref); }
     __device__ __forceinline__ float distance(float x) const { return kMixed ? fmaf(x, kLog2e, -r2) : (x - r) * kLog2e; }
-    __device__ __forceinline__ void add(float x) {
-        const float t = distance(x), e = __builtin_amdgcn_exp2f(t);
+    // skip: x counts as nothing
+    __device__ __forceinline__ void add(float x, bool skip = false) {
+        const float t = distance(x), e = skip ? 0.f : __builtin_amdgcn_exp2f(t);
         s += e;
         st = fmaf(e, fmaxf(t, kFloor), st);
     }
@@ -117,6 +122,34 @@ struct LaneSum {
     }
 };
 
+// The largest element, and the others in any order.  NaN stays among the others.
+__device__ __forceinline__ float split(const Granule<float> &g, float *low) {
+    float hi[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        hi[j] = __builtin_elementwise_maximum(g.v[j], g.v[j + 2]);
+        low[j] = __builtin_elementwise_minimum(g.v[j], g.v[j + 2]);
+    }
+    low[2] = __builtin_elementwise_minimum(hi[0], hi[1]);
+    return fmaxf(hi[0], hi[1]);
+}
+__device__ __forceinline__ float split(const Granule<half_t> &g, float *low) {
+    half2_t x[4], l[3];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = half2_t{g.v[2 * j], g.v[2 * j + 1]};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        l[j] = __builtin_elementwise_minimum(x[j], x[j + 2]);
+        x[j] = __builtin_elementwise_maximum(x[j], x[j + 2]);
+    }
+    l[2] = __builtin_elementwise_minimum(x[0], x[1]);
+    x[0] = __builtin_elementwise_maximum(x[0], x[1]);
+#pragma unroll
+    for (int j = 0; j < 6; ++j) low[j] = (float)l[j / 2][j % 2];
+    low[6] = (float)__builtin_elementwise_minimum(x[0][0], x[0][1]);
+    return fmaxf((float)x[0][0], (float)x[0][1]);
+}
+
 template <typename E>
 __device__ __forceinline__ float largest(const Granule<E> &g) {
     float c = -INFINITY;
@@ -134,17 +167,32 @@ __device__ __forceinline__ float wave_max(float v) {
     return fmaxf(v, __shfl_xor(v, 32, kWave));
 }
 
+// Sums about the rounded M log2 e, in base 2, as sums about M log2 e
+__device__ __forceinline__ void about_exactly(float M, float *s, float *st) {
+    if (fabsf(M) == INFINITY) return;
+    const float off = fmaf(-M, kLog2e, M * kLog2e), f = __builtin_amdgcn_exp2f(off);
+    *st = fmaf(off, *s, *st) * f;
+    *s *= f;
+}
+
+// log(1 + u), u >= 0, to its relative precision: u' = (1 + u) - 1 is what the logarithm saw of u (Kahan's correction)
+__device__ __forceinline__ float log_above_one(float u) {
+    const float one = 1.f + u, seen = one - 1.f;
+    return seen > 0.f ? logf(one) * (u / seen) : u;
+}
+
 // What a row's sums mean.  NaN or +inf among the logits: everything NaN; nothing above -inf: nothing has a probability.
 struct RowStats {
     float m, log_sum, entropy;
     bool bad, empty;
-    // sums about M, in base 2; mixed: about the rounded M log2 e
-    __device__ RowStats(float M, float s, float st, bool mixed) {
-        bad = !(s == s);
-        empty = s == 0.f;
-        const float nan = quiet_nan(), ln = logf(s), off = mixed ? fmaf(-M, kLog2e, M * kLog2e) : 0.f;
-        log_sum = bad ? nan : empty ? -INFINITY : fmaf(off, kLn2, ln);
-        entropy = bad ? nan : empty ? 0.f : fmaxf(ln - kLn2 * (st / s), 0.f);
+    // M: the row's largest logit, `tops` times; s, st: the sums of the others about it, in base 2.  S = tops + s, and what S has
+    // above 1 is held by itself: of a confident row it is all that log S, and minus the best token's log probability, consist of.
+    __device__ RowStats(float M, float tops, float s, float st) {
+        bad = !(s == s) || M == INFINITY;
+        empty = M == -INFINITY;
+        const float nan = quiet_nan(), above = s + (tops - 1.f), ln = log_above_one(above);
+        log_sum = bad ? nan : empty ? -INFINITY : ln;
+        entropy = bad ? nan : empty ? 0.f : ln - kLn2 * (st / (1.f + above));
         m = bad ? nan : M;
     }
     __device__ float log_prob(float x) const { return bad ? quiet_nan() : empty ? -INFINITY : (x - m) - log_sum; }
@@ -264,16 +312,19 @@ struct RowEnd {
     // (room for every wavefront's best, and for rows that have fewer granules than there are alternatives)
     static constexpr int kMost = WAVES < 8 ? 8 * SPECEE_TOP_MAX : WAVES * SPECEE_TOP_MAX;
     float s[WAVES], st[WAVES];
+    int tops[WAVES];
     int entries;  // 0 at a meeting of the workgroup before the first candidate; more than kMost: some had no place
     float v[kMost];
     int id[kMost];
 
-    __device__ __forceinline__ void sums(float sum, float sumt) {
+    // of a wavefront: lanes' sums without what equals the maximum, and how often that was
+    __device__ __forceinline__ void sums(float sum, float sumt, int top) {
         sum = wave_sum(sum);
         sumt = wave_sum(sumt);
         if ((threadIdx.x & (kWave - 1)) == 0) {
             s[threadIdx.x / kWave] = sum;
             st[threadIdx.x / kWave] = sumt;
+            tops[threadIdx.x / kWave] = top;
         }
     }
     // Places for c entries of a wavefront
@@ -320,9 +371,9 @@ struct RowEnd {
     // place (they nearly always do: without equal logits K alternatives have about K to 1.5 K of them); else each wavefront's
     // best.  Follows and ends with a meeting.
     template <bool MANY, typename F>
-    __device__ __forceinline__ void gather(float tau, int K, float sum, float sumt, const F &each) {
+    __device__ __forceinline__ void gather(float tau, int K, float sum, float sumt, int top, const F &each) {
         if (MANY) {
-            sums(sum, sumt);
+            sums(sum, sumt, top);
             each(*this, tau);
             __syncthreads();
             if (entries <= kMost) return;
@@ -330,29 +381,33 @@ struct RowEnd {
             if (threadIdx.x == 0) entries = 0;
             __syncthreads();
         }
-        TopList top;
-        each(top, tau);
-        if (!MANY) sums(sum, sumt);
-        leave(top, K);
+        TopList list;
+        each(list, tau);
+        if (!MANY) sums(sum, sumt, top);
+        leave(list, K);
         __syncthreads();
     }
-    // Behind a meeting: the row's or the part's outputs.  An entry's place is its rank.
-    template <typename E>
+    // Behind a meeting: the row's outputs, or what a PART of one leaves.  An entry's place is its rank.
+    template <bool PART, typename E>
     __device__ __forceinline__ void write(const LogprobsParams &p, int n, int part, const E *row, float M) const {
         const int tid = threadIdx.x;
         float S = 0.f, ST = 0.f;
+        int top = 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             S += s[w];
             ST += st[w];
+            top += tops[w];
         }
-        const RowStats stats(M, S, ST, LaneSum<E>::kMixed);
+        if (LaneSum<E>::kMixed) about_exactly(M, &S, &ST);
+        const RowStats stats(M, (float)top, S, ST);
         const size_t at = (size_t)n * p.parts + part;
-        if (p.parts > 1) {
+        if (PART) {
             if (tid == 0) {
                 p.part_sums[at * 4] = M;
                 p.part_sums[at * 4 + 1] = S;
                 p.part_sums[at * 4 + 2] = ST;
+                p.part_sums[at * 4 + 3] = (float)top;
             }
         } else {
             if (tid == 0) write_row(p, n, stats);
@@ -361,7 +416,7 @@ struct RowEnd {
         if (p.K == 0) return;
         const int C = entries;
         auto put = [&](int k, float x, int i) {
-            if (p.parts > 1) {
+            if (PART) {
                 p.part_vals[at * p.K + k] = x;
                 p.part_ids[at * p.K + k] = i;
             } else {
@@ -424,6 +479,7 @@ __global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) 
         // (fp16 logits are widened again below: kept as floats they would cost half of the workgroups that a CU holds)
         if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
     }
+    const float mine = c;
     c = Group::max(c);
     if (tid % Group::lanes == 0) groups[tid / Group::lanes] = c;
     __syncthreads();
@@ -431,17 +487,31 @@ __global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) 
     if (p.K) kth_largest<Group::n, WAVES>(c, p.K, &tau);
     const float M = wave_max(c);
     LaneSum<E> a(fmaxf(M, LaneSum<E>::kLowest));
+    int tops = 0;
+    auto add = [&](float x, auto with_top) {
+        const bool top = with_top && x == M;
+        if (with_top) tops += __popcll(__ballot(top));
+        a.add(x, top);
+    };
+    auto add_all = [&](auto with_top) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const Granule<E> x = __builtin_bit_cast(Granule<E>, raw[u]);
+        for (int u = 0; u < U; ++u) {
+            const Granule<E> x = __builtin_bit_cast(Granule<E>, raw[u]);
 #pragma unroll
-        for (int j = 0; j < G; ++j) a.add((float)x.v[j]);
-        if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
+            for (int j = 0; j < G; ++j) add((float)x.v[j], with_top);
+            if (sizeof(E) == 2) asm volatile("" : "+v"(raw[u]));
+        }
+        add(xe, with_top);
+    };
+    if (__ballot(mine == M)) {
+        asm volatile("" : "+v"(a.r), "+v"(a.r2));  // (differences formed once for both ways would not fit the registers)
+        add_all(std::true_type());
+    } else {
+        add_all(std::false_type());
     }
-    a.add(xe);
     if (p.K) {
         __syncthreads();
-        last.template gather<MANY>(tau, p.K, a.s, a.st, [&](auto &to, float least) {
+        last.template gather<MANY>(tau, p.K, a.s, a.st, tops, [&](auto &to, float least) {
             if (wave == 0 && heads) to.template scan<1>(&xe, xe, lane, lane < heads, least, p.K);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
@@ -453,14 +523,15 @@ __global__ __launch_bounds__(kT, 8) void logprobs_held_kernel(LogprobsParams p) 
                 to.template scan<1>(&xe, xe, p.V - row.tail + lane - heads, lane >= heads && lane < heads + tails, least, p.K);
         });
     } else {
-        last.sums(a.s, a.st);
+        last.sums(a.s, a.st, tops);
         __syncthreads();
     }
-    last.write(p, n, part, row.p, M);
+    last.template write<true>(p, n, part, row.p, M);
 }
 
-// A row of any length, in steps.  A lane keeps the place of its largest granule and the maximum of the others: behind the pass
-// the lanes whose largest reaches tau read that granule again, and the few of which another does, all of theirs.
+// A row of any length, in steps.  A lane keeps its largest element, out of its sums, its place, and the maximum of the other
+// granules.  Behind the pass the row's maximum is known, and what equals it stays out of the sums for good; the lanes whose
+// largest reaches tau read its granule again, and the few of which another does, all of theirs.
 template <typename E, int T, bool MANY>
 __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
     constexpr int G = Granule<E>::n, WAVES = T / kWave;
@@ -476,11 +547,13 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
     float best = -INFINITY, others = -INFINITY;
     int place = 0;
     auto take = [&](const Granule<E> &x, int g) {
-        const float c = largest(x);
+        float low[G];
+        const float c = split(x, low), less = fminf(c, best);
         a.raise(c);
+        a.add(less);
 #pragma unroll
-        for (int j = 0; j < G; ++j) a.add((float)x.v[j]);
-        others = fmaxf(others, fminf(c, best));
+        for (int j = 0; j < G - 1; ++j) a.add(low[j]);
+        others = fmaxf(others, less);
         place = c > best ? g : place;
         best = fmaxf(best, c);
     };
@@ -509,11 +582,7 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
     }
     const bool extra = tid < row.head + row.tail;
     float xe = -INFINITY;
-    if (extra) {
-        xe = (float)(tid < row.head ? row.p[tid] : end[tid - row.head]);
-        a.raise(xe);
-        a.add(xe);
-    }
+    if (extra) xe = (float)(tid < row.head ? row.p[tid] : end[tid - row.head]);
     if (tid == 0) last.entries = 0;
     float c = Group::max(fmaxf(best, xe == xe ? xe : -INFINITY));
     if (tid % Group::lanes == 0) groups[tid / Group::lanes] = c;
@@ -522,9 +591,17 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
     const float M = wave_max(c);
     if (p.K) kth_largest<Group::n, WAVES>(c, p.K, &tau);
     a.move(M);
+    int tops = 0;
+    auto rest = [&](float x) {
+        const bool top = x == M;
+        tops += __popcll(__ballot(top));
+        a.add(x, top);
+    };
+    rest(best);
+    rest(xe);
     if (p.K) {
         __syncthreads();
-        last.template gather<MANY>(tau, p.K, a.s, a.st, [&](auto &to, float least) {
+        last.template gather<MANY>(tau, p.K, a.s, a.st, tops, [&](auto &to, float least) {
             to.template scan<1>(&xe, xe, tid < row.head ? tid : p.V - row.tail + tid - row.head, extra, least, p.K);
             const bool several = others >= least && others > -INFINITY;
             if (__ballot(best >= least && best > -INFINITY && !several)) {
@@ -546,10 +623,10 @@ __global__ __launch_bounds__(T, 8) void logprobs_kernel(LogprobsParams p) {
             }
         });
     } else {
-        last.sums(a.s, a.st);
+        last.sums(a.s, a.st, tops);
         __syncthreads();
     }
-    last.write(p, n, 0, row.p, M);
+    last.template write<false>(p, n, 0, row.p, M);
 }
 
 // Joins the parts of a row.  A thread holds one of their candidates, as an integer of the same order (by logit, where the two
@@ -573,18 +650,23 @@ __global__ __launch_bounds__(2 * kJoinMost) void logprobs_join_kernel(LogprobsPa
         above[tid] = 0;
     }
     if (tid == 0) real = 0;
-    float r = -INFINITY;
-    LaneSum<E> a(0.f);
+    float r = -INFINITY, tops = 0.f;
+    LaneSum<float> a(0.f);
     if (lane < p.parts) {
         const float *sums = p.part_sums + ((size_t)n * p.parts + lane) * 4;
         r = sums[0];
         a.about(r);
         a.s = sums[1];
         a.st = sums[2];
+        tops = sums[3];
     }
     const float M = wave_max(r);
+    if (r != M) {  // a part's maxima that are not the row's; of a part of -inf alone they are nothing
+        if (r > -INFINITY) a.s += tops;
+        tops = 0.f;
+    }
     a.move(M);
-    const RowStats st(M, wave_sum(a.s), wave_sum(a.st), LaneSum<E>::kMixed);
+    const RowStats st(M, wave_sum(tops), wave_sum(a.s), wave_sum(a.st));
     if (tid == 0) write_row(p, n, st);
     write_tokens(p, n, row, st, tid);
     if (p.K == 0) return;

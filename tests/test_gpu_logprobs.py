@@ -235,6 +235,106 @@ def test_graph_replays_and_two_streams(sp, N, V, n_top):
         assert torch.equal(dx, rg)
 
 
+# ---- confident rows ---------------------------------------------------------------------------------------------------
+
+# each kernel and way of dealing rows out: rows in steps by 256, 512 and 1024 threads, rows in parts of four and of eight
+# granules per thread
+CONFIDENT = [(1100, 777), (300, 4100), (600, 9001), (200, 32003), (60, 128256), (24, 200001), (9, 60001)]
+
+
+def confident(N, V, dtype, seed):
+    """Rows whose largest logit stands by itself, `gap` above the log of the sum of the others: from -1 (no confidence) to 60; a
+    few rows about 1000 and -3000, one with the largest twice."""
+    x = logits(N, V, torch.float32, seed, std=1.0)
+    gap = torch.linspace(-1.0, 60.0, N)
+    at = torch.randint(0, V, (N,), generator=torch.Generator().manual_seed(seed + 1))
+    at[:3] = torch.tensor([0, V - 1, 1])
+    x[torch.arange(N), at] = torch.logsumexp(x, 1) + gap
+    x[4::9] += 1000.0
+    x[6::9] -= 3000.0
+    x[N // 2, (at[N // 2] + V // 2) % V] = x[N // 2, at[N // 2]]
+    return x.to(dtype)
+
+
+def above_one(x):
+    """(S - 1, sum of e * (M - x)) in 64 bits: one of the largest stays out of the sum."""
+    z = x.double()
+    M, at = z.max(1, keepdim=True)
+    e = (z - M).exp()
+    e.scatter_(1, at, 0.0)
+    return e.sum(1), torch.where(e > 0, e * (M - z), torch.zeros_like(e)).sum(1)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("n_top", [0, 3, 12])
+@pytest.mark.parametrize("N,V", CONFIDENT)
+def test_confident_rows_keep_their_relative_precision(sp, N, V, n_top, dtype):
+    """log S = log(1 + u), u the sum over all but one of the largest, entropy = log S + (sum of e a) / S, a = M - x: sums of terms
+    above 0, so the relative error is that of the terms and of adding up.  A term exp(-a) is formed about a reference up to 8 off
+    and moved to M: its exponents, up to a + 16 in all, are each rounded three times (difference, constant, product), which is
+    2.5 steps of 2^-24 of them, and two exponentials and their product are 5 steps; rescaled by every rise of the reference, one per
+    8 of a lane's spread (four at most here: std 1), 5 steps each.  Adding up: V / 512 + 64 steps.  The logarithm and the division:
+    6 steps.  In the sum of e a, a itself is the difference of two such exponents: 3 * (a + 24) steps of 1 more, on the part
+    that this sum has of the entropy."""
+    x = confident(N, V, dtype, 5)
+    u, ua = above_one(x)
+    log_sum = torch.log1p(u)
+    H = log_sum + ua / (1 + u)
+    out = sp.logprobs(x.cuda(), x.argmax(1, keepdim=True).int().cuda(), n_top=n_top)
+    got = {k: v.double().cpu() for k, v in out.items() if k != "_workspace"}
+    steps = V / 512 + 64 + 2.5 * (ua / u + 16) + 5 * 5 + 6
+    assert bool((got["log_sum"] >= 0).all()) and bool((got["entropy"] >= 0).all())
+    off = (got["log_sum"] - log_sum).abs() / log_sum
+    assert bool((off <= steps * EPS).all()), (float(off.max()), int(off.argmax()))
+    off = (got["entropy"] - H).abs()
+    lim = (steps * H + 3 * (ua + 24 * u) / (1 + u)) * EPS
+    assert bool((off <= lim).all()), (float((off / H).max()), int((off / H).argmax()))
+    assert torch.equal(got["logprobs"][:, 0], -got["log_sum"])
+    if n_top:
+        assert torch.equal(got["top_logprobs"][:, 0], -got["log_sum"])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("n_top", [0, 3, 12])
+@pytest.mark.parametrize("N,V", CONFIDENT)
+def test_one_allowed_token_is_certain(sp, N, V, n_top, dtype):
+    """As a grammar leaves a row: its log probability, log S and the entropy are 0, whatever the logit."""
+    gen = torch.Generator().manual_seed(N)
+    x = torch.full((N, V), -INF, dtype=dtype)
+    ids = torch.randint(0, V, (N, 1), generator=gen)
+    x.scatter_(1, ids, (torch.randn((N, 1), generator=gen) * 10.0 ** torch.linspace(-2, 4, N)[:, None]).to(dtype))
+    out = sp.logprobs(x.cuda(), ids.int().cuda(), n_top=n_top)
+    for k in ("log_sum", "entropy", "logprobs"):
+        assert not bool(out[k].any()), (k, float(out[k].abs().max()))
+    assert torch.equal(out["max_logit"].cpu(), x.gather(1, ids)[:, 0].float())
+    if n_top:
+        assert torch.equal(out["top_ids"][:, :1].cpu().long(), ids) and not bool(out["top_logprobs"][:, 0].any())
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("N,V", CONFIDENT)
+def test_the_largest_many_times(sp, N, V, dtype):
+    """S is their number where all else is forbidden, and log S and the entropy are its logarithm.  Of fp32 logits every term is
+    exactly 1 and S a whole number: 6 steps of the logarithm.  Of fp16 logits the terms and their scale are off by two steps
+    each, and adding them up rounds V / 512 + 64 times."""
+    gen = torch.Generator().manual_seed(N)
+    x = torch.full((N, V), -INF, dtype=dtype)
+    count = torch.randint(1, V, (N,), generator=gen)
+    count[:3] = torch.tensor([2, 3, V])
+    value = (torch.randn((N,), generator=gen) * 30).to(dtype)
+    for n in range(N):
+        x[n, torch.randperm(V, generator=gen)[:count[n]]] = value[n]
+    out = sp.logprobs(x.cuda(), n_top=2)
+    want = count.double().log()
+    for k in ("log_sum", "entropy"):
+        off = (out[k].double().cpu() - want).abs()
+        lim = 6 * EPS * want + (0.0 if dtype == torch.float32 else (V / 512 + 64 + 4) * EPS * (count > 1))
+        assert bool((off <= lim).all()), (k, float(off.max()))
+
+
 # ---- gradient ---------------------------------------------------------------------------------------------------------
 
 def plain_grad(x, ids, g, gh):
