@@ -694,7 +694,8 @@ constexpr int kGradSteps = 4;
 struct GradRow {
     float m, log_sum, entropy, factor, g_entropy;
     __device__ __forceinline__ float operator()(float x) const {
-        const float lp = fmaxf((x - m) - log_sum, -200.f);  // exp(-200) is 0
+        // (exp(-200) is 0; a NaN, which m and log_sum of a row without meaning are, stays one)
+        const float lp = __builtin_elementwise_maximum((x - m) - log_sum, -200.f);
         return -__builtin_amdgcn_exp2f(lp * kLog2e) * fmaf(g_entropy, lp + entropy, factor);
     }
 };

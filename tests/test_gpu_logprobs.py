@@ -418,6 +418,23 @@ def test_gradient_of_rows_that_are_special(sp, what, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("T", [0, 3])
+@pytest.mark.parametrize("N,V", [(3, 4099), (600, 515), (520, 3)])
+@pytest.mark.parametrize("what", sorted(ROWS))
+def test_gradient_of_special_rows_without_entropy(sp, what, N, V, T, dtype):
+    """The ordinary loss, of log probabilities alone: a row with NaN or +inf has no gradient but NaN, its tokens' too."""
+    x = logits(N, V, dtype, 17)
+    ROWS[what](x)
+    ids = tokens(N, V, T, 5)
+    g = torch.randn((N, T), generator=torch.Generator().manual_seed(9))
+    y = x.cuda()
+    st = sp.logprobs(y)
+    got = sp.logprobs_grad(y, ids.cuda() if T else None, st["max_logit"], st["log_sum"], g_logprobs=g.cuda() if T else None)
+    check_grad(got, x, ids, g, None)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 def test_gradient_strides_alignments_and_places(sp, dtype):
     N, V = 3, 2053
     x, ids = logits(N, V, dtype, 2), tokens(N, V, 2, 5)
