@@ -687,16 +687,31 @@ __global__ __launch_bounds__(2 * kJoinMost) void logprobs_join_kernel(LogprobsPa
     if (tid >= real && tid < p.K) write_alternative(p, n, tid, st, -INFINITY, INT_MAX);
 }
 
-// Gradient: elementwise, one workgroup per kGradSteps * T granules of a row; the ids that fall into its share are looked
-// for once and kept in LDS, in their order, so that ids that repeat add up the same way every time.
+// Gradient: elementwise, one workgroup per kGradSteps * T granules of a row; the ids that fall into its share are looked for
+// once and kept in LDS, each with the sum of its gradients, in their order.  At an id the definition is a difference, of g and
+// p g of the same token, which is all that a confident target has: it is formed as g (1 - p) by itself.
 constexpr int kGradSteps = 4;
 
 struct GradRow {
     float m, log_sum, entropy, factor, g_entropy;
+    // (exp(-200) is 0; a NaN, which m and log_sum of a row without meaning are, stays one)
+    __device__ __forceinline__ float log_prob(float x) const {
+        return __builtin_elementwise_maximum((x - m) - log_sum, -200.f);
+    }
+    // factor: the sum of the gradients of all tokens' log probabilities, or of those of the others
+    __device__ __forceinline__ float by_others(float p, float lp, float others) const {
+        return -p * fmaf(g_entropy, lp + entropy, others);
+    }
     __device__ __forceinline__ float operator()(float x) const {
-        // (exp(-200) is 0; a NaN, which m and log_sum of a row without meaning are, stays one)
-        const float lp = __builtin_elementwise_maximum((x - m) - log_sum, -200.f);
-        return -__builtin_amdgcn_exp2f(lp * kLog2e) * fmaf(g_entropy, lp + entropy, factor);
+        const float lp = log_prob(x);
+        return by_others(__builtin_amdgcn_exp2f(lp * kLog2e), lp, factor);
+    }
+    // 1 - p to its relative precision: log p over what the logarithm of the rounded p is (Kahan's correction)
+    __device__ __forceinline__ float at_id(float x, float g, float others) const {
+        const float lp = log_prob(x), p = __builtin_amdgcn_exp2f(lp * kLog2e);
+        float rest = 1.f - p;
+        if (p > 0.5f) rest = rest > 0.f ? rest * (lp * kLog2e) * __builtin_amdgcn_rcpf(__builtin_amdgcn_logf(p)) : -lp;
+        return fmaf(g, rest, by_others(p, lp, others));
     }
 };
 
@@ -713,7 +728,7 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
     const int v0 = first ? 0 : row.index(g0), v1 = last ? p.V : row.index(g1);
 
     __shared__ int hit_id[SPECEE_IDS_MAX], hits;
-    __shared__ float hit_g[SPECEE_IDS_MAX], factor;
+    __shared__ float hit_g[SPECEE_IDS_MAX], hit_others[SPECEE_IDS_MAX], factor;
     if (tid < kWave) {
         int id = -1;
         float gt = 0.f;
@@ -722,12 +737,22 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
             if ((unsigned)id < (unsigned)p.V) gt = p.g_logprobs[(size_t)n * p.T + lane];
         }
         const float sum = wave_sum(gt);
-        const bool here = id >= v0 && id < v1;
+        float same = 0.f, others = 0.f;
+        bool repeated = false;
+        for (int t = 0; t < p.T; ++t) {
+            const bool eq = __builtin_amdgcn_readlane(id, t) == id;
+            const float g = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, gt), t));
+            same += eq ? g : 0.f;
+            others += eq ? 0.f : g;
+            repeated |= eq && t < lane;
+        }
+        const bool here = id >= v0 && id < v1 && !repeated;
         const unsigned long long who = __ballot(here);
         if (here) {
             const int at = __popcll(who & ((1ull << lane) - 1));
             hit_id[at] = id;
-            hit_g[at] = gt;
+            hit_g[at] = same;
+            hit_others[at] = others;
         }
         if (lane == 0) {
             hits = __popcll(who);
@@ -767,9 +792,14 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
             for (int j = 0; j < G; ++j) d[j] = f((float)x[u].v[j]);
             for (int h = 0; h < H; ++h) {
                 const int j0 = hit_id[h] - at;
-                if ((unsigned)j0 < (unsigned)G)
+                if ((unsigned)j0 < (unsigned)G) {
+                    float xh = 0.f;
 #pragma unroll
-                    for (int j = 0; j < G; ++j) d[j] += j == j0 ? hit_g[h] : 0.f;
+                    for (int j = 0; j < G; ++j) xh = j == j0 ? (float)x[u].v[j] : xh;
+                    const float dh = f.at_id(xh, hit_g[h], hit_others[h]);
+#pragma unroll
+                    for (int j = 0; j < G; ++j) d[j] = j == j0 ? dh : d[j];
+                }
             }
             Granule<E> o;
 #pragma unroll
@@ -786,7 +816,8 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
     }
     if (extra >= 0) {
         float d = f(xe);
-        for (int h = 0; h < H; ++h) d += hit_id[h] == extra ? hit_g[h] : 0.f;
+        for (int h = 0; h < H; ++h)
+            if (hit_id[h] == extra) d = f.at_id(xe, hit_g[h], hit_others[h]);
         out[extra] = (E)(empty ? 0.f : d);
     }
 }

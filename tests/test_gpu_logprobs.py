@@ -435,6 +435,29 @@ def test_gradient_of_special_rows_without_entropy(sp, what, N, V, T, dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+@pytest.mark.parametrize("repeats", [1, 2, 5])
+@pytest.mark.parametrize("N,V", [(600, 515), (40, 515), (60, 32003)])
+def test_gradient_of_a_confident_target(sp, N, V, repeats, dtype):
+    """The target is the best token, alone or named several times: g (1 - p) there, whose relative error is that of log p
+    (test_confident_rows_keep_their_relative_precision) and 6 steps more, and of the sum of the g, which are of one sign."""
+    x = confident(N, V, dtype, 7)
+    u, ua = above_one(x)
+    g = torch.rand((N, repeats), generator=torch.Generator().manual_seed(3)) + 0.5
+    ids = x.argmax(1, keepdim=True).int().expand(N, repeats).contiguous()
+    y = x.cuda()
+    st = sp.logprobs(y)
+    got = sp.logprobs_grad(y, ids.cuda(), st["max_logit"], st["log_sum"], g_logprobs=g.cuda()).double().cpu()
+    got = got.gather(1, ids[:, :1].long())[:, 0]
+    want = g.double().sum(1) * u / (1 + u)
+    lim = (V / 512 + 64 + 2.5 * (ua / u + 16) + 5 * 5 + 6 + 6 + repeats) * EPS * want
+    if dtype == torch.float16:
+        lim = lim + 2.0 ** -11 * want + 2.0 ** -25
+    off = (got - want).abs()
+    assert bool((off <= lim).all()), (float((off / want).max()), int((off / lim).argmax()))
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 def test_gradient_strides_alignments_and_places(sp, dtype):
     N, V = 3, 2053
     x, ids = logits(N, V, dtype, 2), tokens(N, V, 2, 5)
