@@ -377,7 +377,7 @@ int specee_block_norm(const specee_dims *dims, int N, const specee_half *hidden,
  * from the codes on the 8-bit matrix cores, which line products of 128 elements up with the largest of them: off by 1e-5 to
  * 5e-5 of the 2-norm of a block's products (up to 4e-4 for single sums), where fp16 rounds by up to 5e-4.
  * d: a multiple of 16, at most 65536; only dims->d and dims->V are read.
- * Workspace: SPECEE_OP_MATMUL_F8 with n = N.
+ * Workspace: SPECEE_OP_MATMUL_F8 with n = N, or the largest N that is to come.
  */
 int specee_matmul_f8(const specee_dims *dims, int N, const specee_f8 *x, const float *x_scales, const specee_f8 *weight,
                      const float *w_scales, float *out, specee_half *out_f16, void *workspace, size_t workspace_bytes,
@@ -398,7 +398,8 @@ int specee_matmul_f8(const specee_dims *dims, int N, const specee_f8 *x, const f
  * Rows and ids that mean nothing: a row of -inf alone has m, log S and every log probability -inf and entropy 0;
  * a NaN or +inf in a row makes all its outputs NaN, its top_ids -1; the log probability of an id outside
  * [0, V) is NaN.
- * Only dims->V is read.  Workspace: SPECEE_OP_LOGPROBS with n = N and n_top in the place of Mcap.  N <= 65535.
+ * Only dims->V is read.  Workspace: SPECEE_OP_LOGPROBS with n = N and n_top in the place of Mcap, or
+ * the largest of each that are to come.  N <= 65535.
  */
 int specee_logprobs(const specee_dims *dims, int N, const float *logits, const specee_half *logits_f16,
                     long long stride, const int32_t *ids, int T, int n_top, float *logprobs, float *max_logit,

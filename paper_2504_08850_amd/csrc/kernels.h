@@ -237,6 +237,7 @@ struct MatmulF8Params {
     void *workspace;
 };
 size_t matmul_f8_workspace(int N, int V, int d);
+size_t matmul_f8_workspace_up_to(int most, int V, int d);
 hipError_t launch_matmul_f8(const MatmulF8Params &p, bool half, hipStream_t s);
 
 // Log probabilities of rows of logits, fp32 or fp16, and their gradient (logprobs.hip)
@@ -259,6 +260,7 @@ struct LogprobsGradParams {
     void *grad;
     bool once;  // set by the launcher: gradients too large for any cache
 };
+constexpr int kLogprobsRowsInParts = 64;  // more rows are never cut into parts
 int logprobs_parts(int N, int V, bool half);
 hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s);
 hipError_t launch_logprobs_grad(const LogprobsGradParams &p, bool half, hipStream_t s);

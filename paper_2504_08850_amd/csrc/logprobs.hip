@@ -836,7 +836,7 @@ struct Deal {
 };
 Deal deal(int N, int V, bool half) {
     const int whole = V / (half ? 8 : 4), most = (half ? 4 : 8) * kT;  // (8 of fp16 leave the registers)
-    if (N > 0 && N <= 64 && whole > 14336 && whole <= kMaxParts * (most - 1)) {
+    if (N > 0 && N <= kLogprobsRowsInParts && whole > 14336 && whole <= kMaxParts * (most - 1)) {
         int parts = std::min(512 / N, kMaxParts);
         while ((whole + parts - 1) / parts + 1 > most) ++parts;
         return Deal{parts, kT, (whole + parts - 1) / parts + 1 <= 4 * kT ? 4 : 8};

@@ -582,6 +582,16 @@ size_t matmul_f8_workspace(int N, int V, int d) {
     return parts > 1 ? (size_t)parts * N * V * sizeof(float) : 0;
 }
 
+// Every N from 1 to `most`: shape_of answers the same from one multiple of 32 (or 16) up to the next, so the largest N of each
+// such range is asked for, from the largest that may have parts down to where eight of them could not need more.
+size_t matmul_f8_workspace_up_to(int most, int V, int d) {
+    size_t need = matmul_f8_workspace(most, V, d);
+    const int high = (int)std::min<long>(most, 128l * 256 / ((V + 511) / 512));  // (no tile is larger, and parts have at most 128)
+    for (int N = high / 32 * 32; N >= 32 && (size_t)8 * N * V * sizeof(float) > need; N -= 32)
+        need = std::max(need, matmul_f8_workspace(N, V, d));
+    return std::max(need, matmul_f8_workspace(std::min(most, 16), V, d));
+}
+
 hipError_t launch_matmul_f8(const MatmulF8Params &p, bool half, hipStream_t s) {
     const Shape sh = shape_of(p.N, p.V, p.d, half);
     return half ? launch_shape<half_t>(p, sh, s) : launch_shape<float>(p, sh, s);

@@ -225,10 +225,15 @@ size_t specee_workspace_bytes(int op, const specee_dims *dm, int n, int Mcap) {
                                                 ? head_states_workgroups(dm->d, dm->V, dm->d % 128 == 0 ? 128 : 64, INT_MAX)
                                                 : 0));
         case SPECEE_OP_MATMUL_F8:
-            return check_f8(dm, n) ? (size_t)-1 : matmul_f8_workspace(n, dm->V, dm->d);
-        case SPECEE_OP_LOGPROBS:
+            return check_f8(dm, n) ? (size_t)-1 : matmul_f8_workspace_up_to(n, dm->V, dm->d);
+        case SPECEE_OP_LOGPROBS: {
             if (!dm || dm->V < 1 || n > 65535 || Mcap < 0 || Mcap > SPECEE_TOP_MAX) return (size_t)-1;
-            return logprobs_layout(n, std::max(logprobs_parts(n, dm->V, false), logprobs_parts(n, dm->V, true)), Mcap).total;
+            size_t need = 0;  // of up to n rows: more of them may be in fewer parts, or in one
+            for (int rows = std::min(n, kLogprobsRowsInParts); rows > 0; --rows)
+                need = std::max(need, logprobs_layout(rows, std::max(logprobs_parts(rows, dm->V, false),
+                                                                     logprobs_parts(rows, dm->V, true)), Mcap).total);
+            return need;
+        }
         case SPECEE_OP_LAYER_LOOP:
             if (check_dims(dm, true) || n > kLoopMaxTokens) return (size_t)-1;
             return loop_layout(n).total;

@@ -544,6 +544,25 @@ def test_refusals_without_a_gpu(sp):
     assert 0 < sp.workspace_bytes(sp.OP_LOGPROBS, sp.Dims(8, 128256, 1, 1, 0.0, 0.5), 1, 32) < 1 << 14
 
 
+@pytest.mark.parametrize("n_top", [0, 5, 32])
+@pytest.mark.parametrize("V", [100, 60001, 128256, 200001, 262080, 300007])
+def test_a_workspace_for_many_rows_serves_fewer(sp, V, n_top):
+    dims = sp.Dims(8, V, 1, 1, 0.0, 0.5)
+    sizes = [sp.workspace_bytes(sp.OP_LOGPROBS, dims, n, n_top) for n in range(1, 200)]
+    assert sizes == sorted(sizes)
+    assert sizes[-1] >= sp.workspace_bytes(sp.OP_LOGPROBS, dims, 64, max(n_top - 1, 0))
+
+
+@gpu
+def test_a_workspace_for_many_rows_is_taken_by_fewer(sp):
+    V = 128256
+    ws = torch.empty(sp.workspace_bytes(sp.OP_LOGPROBS, sp.Dims(8, V, 1, 1, 0.0, 0.5), 4096, 20), dtype=torch.uint8, device="cuda")
+    for N, n_top in ((70, 20), (64, 20), (33, 5), (1, 20), (3, 0)):
+        for dtype in (torch.float32, torch.float16):
+            x = logits(N, V, dtype, N)
+            check(sp.logprobs(x.cuda(), n_top=n_top, workspace=ws), x, None, n_top)
+
+
 @gpu
 def test_python_refusals(sp):
     x, ids = torch.zeros((2, 40), device="cuda"), torch.zeros((2, 1), dtype=torch.int32, device="cuda")

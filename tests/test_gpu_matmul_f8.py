@@ -149,6 +149,24 @@ def test_same_bits_graphs_and_streams(sp, N, V, d):
             assert torch.equal(ref, kept["out"])
 
 
+@pytest.mark.parametrize("V,d", [(1, 16), (300, 4096), (1000, 65536), (4096, 4096), (5120, 5120), (8192, 8192), (24001, 4608),
+                                 (50280, 2048), (128256, 8192)])
+def test_a_workspace_for_many_states_serves_fewer(sp, V, d):
+    dims = sp.Dims(d, V, 1, 1, 0.0, 0.5)
+    sizes = [sp.workspace_bytes(sp.OP_MATMUL_F8, dims, n) for n in list(range(1, 700)) + [1000, 2043, 4096, 8192, 40000]]
+    assert sizes == sorted(sizes)
+
+
+@gpu
+def test_a_workspace_for_many_states_is_taken_by_fewer(sp):
+    V, d = 1100, 2064
+    ws = torch.empty(sp.workspace_bytes(sp.OP_MATMUL_F8, sp.Dims(d, V, 1, 1, 0.0, 0.5), 8192), dtype=torch.uint8, device="cuda")
+    for N in (8192, 1, 16, 17, 40, 64, 100, 200, 700):
+        t = inputs(N, V, d, N)
+        for dtype in (torch.float32, torch.float16):
+            check(sp.matmul_f8(**up(t), dtype=dtype, workspace=ws)["out"], t)
+
+
 @gpu
 def test_weights_beyond_32_bits(sp):
     """The last rows of 4.3 GB of weights, and of 4.3 GB of states."""
