@@ -65,6 +65,9 @@ __device__ __forceinline__ floatx4 block_product(const Halves &w, const Halves &
     return c;
 }
 
+// Floats of a part in the workspace: whole quads, so that each part begins at 16 bytes
+__host__ __device__ constexpr size_t part_floats(int N, int V) { return ((size_t)N * V + 3) / 4 * 4; }
+
 template <typename T>
 __device__ __forceinline__ void store_quad(T *out, size_t at, int left, const floatx4 &v) {
     typedef T quad __attribute__((ext_vector_type(4)));
@@ -203,7 +206,7 @@ template <typename T, int I, int J>
 __device__ __forceinline__ void store_tile(const MatmulF8Params &p, const floatx4 (&acc)[I][J], int v0, int n0) {
     const bool parts = gridDim.z > 1;
     const int q = (threadIdx.x & 63) >> 4, c = threadIdx.x & 15;
-    float *part = static_cast<float *>(p.workspace) + (size_t)blockIdx.z * p.N * p.V;
+    float *part = static_cast<float *>(p.workspace) + blockIdx.z * part_floats(p.N, p.V);
 #pragma unroll
     for (int j = 0; j < J; ++j) {
         const int n = n0 + j * 16 + c;
@@ -322,13 +325,13 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
 
 // Sums of the parts, in their order
 template <typename T>
-__global__ __launch_bounds__(256) void matmul_f8_join_kernel(const float *part, int parts, size_t n, T *out) {
+__global__ __launch_bounds__(256) void matmul_f8_join_kernel(const float *part, int parts, size_t stride, size_t n, T *out) {
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= n) return;
     const int left = n - i < 4 ? (int)(n - i) : 4;
     floatx4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < parts; ++s)
-        for (int e = 0; e < left; ++e) sum[e] += part[(size_t)s * n + i + e];
+        for (int e = 0; e < left; ++e) sum[e] += part[s * stride + i + e];
     store_quad(out, i, left, sum);
 }
 
@@ -433,7 +436,7 @@ __global__ __launch_bounds__(1024) void matmul_f8_stream_kernel(MatmulF8Params p
             const int v = (unit * unit_tiles + t) * 16 + 4 * q;
             if (c < p.N && v < p.V) {
                 if (gridDim.y > 1)
-                    store_quad(static_cast<float *>(p.workspace) + (size_t)blockIdx.y * p.N * p.V, (size_t)c * p.V + v,
+                    store_quad(static_cast<float *>(p.workspace) + blockIdx.y * part_floats(p.N, p.V), (size_t)c * p.V + v,
                                p.V - v, sum);
                 else
                     store_quad(static_cast<T *>(p.out), (size_t)c * p.V + v, p.V - v, sum);
@@ -569,7 +572,7 @@ hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s)
     if (e != hipSuccess || sh.parts == 1) return e;
     const size_t n = (size_t)p.N * p.V;
     hipLaunchKernelGGL(matmul_f8_join_kernel<T>, dim3((unsigned)((n + 1023) / 1024)), dim3(256), 0, s,
-                       static_cast<const float *>(p.workspace), sh.parts, n, static_cast<T *>(p.out));
+                       static_cast<const float *>(p.workspace), sh.parts, part_floats(p.N, p.V), n, static_cast<T *>(p.out));
     return hipGetLastError();
 }
 
@@ -579,7 +582,7 @@ hipError_t launch_shape(const MatmulF8Params &p, const Shape &sh, hipStream_t s)
 size_t matmul_f8_workspace(int N, int V, int d) {
     if (N < 1) return 0;
     const int parts = std::max(shape_of(N, V, d, false).parts, shape_of(N, V, d, true).parts);
-    return parts > 1 ? (size_t)parts * N * V * sizeof(float) : 0;
+    return parts > 1 ? parts * part_floats(N, V) * sizeof(float) : 0;
 }
 
 // Every N from 1 to `most`: shape_of answers the same from one multiple of 32 (or 16) up to the next, so the largest N of each
@@ -587,7 +590,7 @@ size_t matmul_f8_workspace(int N, int V, int d) {
 size_t matmul_f8_workspace_up_to(int most, int V, int d) {
     size_t need = matmul_f8_workspace(most, V, d);
     const int high = (int)std::min<long>(most, 128l * 256 / ((V + 511) / 512));  // (no tile is larger, and parts have at most 128)
-    for (int N = high / 32 * 32; N >= 32 && (size_t)8 * N * V * sizeof(float) > need; N -= 32)
+    for (int N = high / 32 * 32; N >= 32 && 8 * part_floats(N, V) * sizeof(float) > need; N -= 32)
         need = std::max(need, matmul_f8_workspace(N, V, d));
     return std::max(need, matmul_f8_workspace(std::min(most, 16), V, d));
 }

@@ -157,6 +157,23 @@ def test_a_workspace_for_many_states_serves_fewer(sp, V, d):
     assert sizes == sorted(sizes)
 
 
+@pytest.mark.parametrize("d", [1296, 2576, 5136])
+def test_parts_are_whole_quads(sp, d):
+    """Results in parts are stored 16 bytes at a time: also where N V is odd each part begins at a multiple of them."""
+    for V in (65, 129, 131, 515):
+        for N in (17, 33, 61, 127, 129):
+            assert sp.workspace_bytes(sp.OP_MATMUL_F8, sp.Dims(d, V, 1, 1, 0.0, 0.5), N) % 16 == 0
+
+
+@gpu
+@pytest.mark.parametrize("N,V,d", [(17, 129, 1296), (61, 131, 2576), (129, 515, 5136), (3, 129, 9360)])
+def test_parts_of_an_odd_number_of_results(sp, N, V, d):
+    t = inputs(N, V, d, 2)
+    want = plain(t)
+    for dtype in (torch.float32, torch.float16):
+        check(sp.matmul_f8(**up(t), dtype=dtype)["out"], t, want)
+
+
 @gpu
 def test_a_workspace_for_many_states_is_taken_by_fewer(sp):
     V, d = 1100, 2064
