@@ -707,7 +707,8 @@ int specee_block_norm(const specee_dims *dm, int N, const specee_half *hidden, c
         return SPECEE_EALIGN;
     BlockNormParams p{};
     p.N = N; p.d = dm->d; p.gate_rows = gate_rows;
-    p.eps = dm->eps; p.hidden_scale = hidden_scale; p.branch_scale = branch_scale;
+    p.eps = dm->eps; p.hidden_scale = hidden_scale;
+    p.branch_scale = branch ? branch_scale : 0.f;  // (without a branch it scales nothing, whatever it is)
     p.hidden = H(hidden); p.branch = H(branch); p.gamma_post = H(gamma_post); p.gate = H(gate); p.gamma = H(gamma);
     p.hidden_out = reinterpret_cast<half_t *>(hidden_out); p.x = reinterpret_cast<half_t *>(x);
     p.x8 = x8; p.x8_scales = x8_scales;

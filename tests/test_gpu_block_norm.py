@@ -101,6 +101,14 @@ def test_without_branch_or_weight(sp):
 
 
 @gpu
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), 3.0])
+def test_without_a_branch_its_scale_means_nothing(sp, scale):
+    t = inputs(4, 1032, 5)
+    t["branch"] = t["gamma_post"] = None
+    check(sp.block_norm(**up(t), branch_scale=scale, want_f8=True), *plain(t), True)
+
+
+@gpu
 def test_rows_of_zeros_and_far_apart_sizes(sp):
     t = inputs(6, 512, 8)
     t["hidden"][2] = 0
