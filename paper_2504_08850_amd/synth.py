@@ -75,14 +75,14 @@ def e4m3(v: np.ndarray) -> np.ndarray:
 def quantize_f8(w: np.ndarray, rows: int = 128):
     """8-bit copy of a matrix [V][d], the storage that specee_matmul_f8 reads: e4m3 codes (uint8 [V][d]) and one fp32 scale
     for every `rows` rows by 128 elements ([ceil(V/rows)][ceil(d/128)]; weights rows = 128, states rows = 1): the largest
-    absolute value of the block / 448, 1 where all of it is 0."""
+    absolute value of the block / 448 (a normal number at least, or it would not divide back), 1 where all of it is 0."""
     V, d = w.shape
     nv, nb = -(-V // rows), -(-d // 128)
     pad = np.zeros((nv * rows, nb * 128), dtype=np.float32)
     pad[:V, :d] = w
     blk = pad.reshape(nv, rows, nb, 128)
     top = np.abs(blk).max(axis=(1, 3))
-    scales = np.where(top > 0, top / np.float32(448.0), np.float32(1.0)).astype(np.float32)
+    scales = np.where(top > 0, np.maximum(top / np.float32(448.0), np.finfo(np.float32).tiny), 1.0).astype(np.float32)
     codes = e4m3(blk / scales[:, None, :, None]).reshape(nv * rows, nb * 128)[:V, :d]
     return np.ascontiguousarray(codes), scales
 

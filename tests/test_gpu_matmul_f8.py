@@ -261,6 +261,17 @@ def test_synthetic_storage_is_e4m3():
     assert np.all(np.abs(back - w) <= np.abs(w) * 2.0 ** -4 * 1.0001 + np.repeat(np.repeat(s, 128, 0)[:130], 128, 1)[:, :200] * 2.0 ** -10)
 
 
+@pytest.mark.parametrize("size", [1e-45, 1e-42, 1e-38, 1e-35, 3e38])
+def test_synthetic_storage_of_blocks_at_the_ends_of_fp32(size):
+    w = (np.random.default_rng(2).uniform(-1, 1, (3, 256)) * size).astype(np.float32)
+    w[0, 0] = w[1, 200] = size
+    q, s = synth.quantize_f8(w)
+    wide = np.repeat(np.repeat(s, 128, 0)[:3], 128, 1).astype(np.float64)
+    back = torch.from_numpy(q).view(F8).float().numpy().astype(np.float64) * wide
+    assert np.isfinite(s).all() and (s >= np.finfo(np.float32).tiny).all()
+    assert np.all(np.abs(back - w) <= np.abs(w) * 2.0 ** -4 * 1.0001 + wide * 2.0 ** -10)
+
+
 def test_refusals_without_a_gpu(sp):
     import ctypes as C
     lib = sp.lib()
