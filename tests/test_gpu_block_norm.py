@@ -136,6 +136,37 @@ def test_in_place_and_outputs_kept(sp):
         assert torch.equal(ref[k].float(), got[k].float()), k
 
 
+# more rows than the GPU holds workgroups for: two to ten turns of each, the last of them uneven
+TURNS = [(600, 16384), (1300, 8200), (2500, 5120), (5001, 4096), (12001, 1032), (41000, 128)]
+
+
+@gpu
+@pytest.mark.parametrize("N,d", TURNS)
+@pytest.mark.parametrize("post,gate", [(True, "none"), (False, "all"), (True, "each"), (None, "none")])
+def test_several_rows_per_workgroup(sp, N, d, post, gate):
+    t = inputs(N, d, N + d, gate, bool(post))
+    if post is None:
+        t["branch"] = None
+    want = plain(t, 0.75, -1.5)
+    for asked in (dict(want_f8=True), dict(want_x=False)):
+        out = sp.block_norm(**up(t), hidden_scale=0.75, branch_scale=-1.5, **asked)
+        check(out, *want, "want_f8" in asked)
+
+
+@gpu
+@pytest.mark.parametrize("N,d", TURNS)
+@pytest.mark.parametrize("gate", ["none", "each"])
+def test_several_rows_per_workgroup_in_place(sp, N, d, gate):
+    t = inputs(N, d, 3, gate)
+    ref = sp.block_norm(**up(t), want_f8=True)
+    for a, b in (("hidden", "branch"), ("branch", "hidden")):      # where the new state and x go
+        u = up(t)
+        out = dict(hidden=u[a], x=u[b], x8=torch.empty_like(ref["x8"]), x8_scales=torch.empty_like(ref["x8_scales"]))
+        sp.block_norm(**u, want_f8=True, out=out)
+        for k in ref:
+            assert torch.equal(ref[k].view(torch.uint8), out[k].view(torch.uint8)), (k, a)
+
+
 @gpu
 def test_neighbouring_memory_is_left_alone(sp):
     N, d = 3, 136
