@@ -82,6 +82,45 @@ def test_against_64_bits(sp, N, V, d):
         check(out, t, want)
 
 
+# every form of tile through at least six blocks of elements, so that loads run ahead of the products, wait their turn and go
+# round, in one part and in several; with a whole last block and with a short one
+STEADY = [(500, 1100, 4112), (600, 300, 16384), (60, 24001, 4608), (40, 8192, 8192), (50, 16500, 2064), (64, 131072, 768),
+          (64, 131072, 784), (50, 33010, 784), (100, 8192, 8192), (100, 9001, 4112), (100, 33010, 784), (300, 5120, 5120),
+          (200, 5200, 5136), (130, 12300, 2576), (4200, 2100, 1024), (4200, 2100, 1040), (4000, 3100, 1024), (4000, 3100, 1040),
+          (2900, 2000, 16400), (2100, 2048, 12304)]
+
+
+@gpu
+@pytest.mark.parametrize("N,V,d", STEADY)
+def test_many_blocks_in_every_form(sp, N, V, d):
+    t = inputs(N, V, d, 11)
+    on = up(t)
+    want = tuple(v.cpu() for v in plain(on))
+    for dtype in (torch.float32, torch.float16):
+        check(sp.matmul_f8(**on, dtype=dtype)["out"], t, want)
+
+
+@gpu
+@pytest.mark.parametrize("N,V,d", [(60, 24001, 4608), (40, 8192, 8192), (64, 131072, 784), (100, 9001, 4112), (300, 5120, 5120),
+                                   (4200, 2100, 1040), (4000, 3100, 1040)])
+def test_many_blocks_give_the_same_bits_in_graphs(sp, N, V, d):
+    t = up(inputs(N, V, d, 12))
+    for dtype in (torch.float32, torch.float16):
+        ref = sp.matmul_f8(**t, dtype=dtype)["out"].clone()
+        kept = sp.matmul_f8(**t, dtype=dtype)
+        assert torch.equal(ref, kept["out"])
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            sp.matmul_f8(**t, dtype=dtype, out=kept["out"], workspace=kept["_workspace"])
+        for _ in range(3):
+            kept["out"].fill_(3)
+            kept["_workspace"].fill_(255)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(ref, kept["out"])
+
+
 @gpu
 @pytest.mark.parametrize("N,V,d", [(1, 300, 4096), (16, 260, 1040), (40, 129, 528), (130, 257, 1168), (300, 300, 2048)])
 def test_every_code(sp, N, V, d):
