@@ -6,15 +6,15 @@
 // itself is in S, and the rest u: where one token is all but certain, log S = log(1 + u) is about u, and S as one number would
 // hold u to 6e-8 of 1 instead of 6e-8 of itself.
 //
-// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 320 us, 6.6
+// Forward: one pass over the logits, bound by their bytes from a few hundred rows on (4096 x 128256 fp32, 2.1 GB: 319 us, 6.6
 // TB/s) and by launch and latency below (1 x 32000: 6.7 us).  A lane keeps its largest element out of its sums, and of the others
 // the sums of exp(x - r) and exp(x - r)(x - r) about a reference r (an element of its own, at most 8 below its maximum): a new
 // maximum seldom costs it a rescaling.  The largest of 16 bytes and the rest come from minima and maxima in pairs, one
 // instruction per element (with S as one number: 1 x 32000 6.4 us, 64 x 128256 14.1 against 14.5, 2043 x 32003 fp16 27.6
-// against 28.6).  16 bytes are loaded per lane and step; rows may start at any element (what lies before the first and behind the
+// against 28.8).  16 bytes are loaded per lane and step; rows may start at any element (what lies before the first and behind the
 // last whole 16 bytes is done one element per lane).  A logit of -inf adds nothing (its t is cut at -300, and 2^-300 is 0 in
 // fp32); NaN makes the sum NaN, +inf is the maximum: both are looked at once at the end.
-// Rows of 64 KB (2043 x 32003 fp16: 28.6 us, 4.6 TB/s) are bound by what each does one after the other, loads, meetings and
+// Rows of 64 KB (2043 x 32003 fp16: 28.8 us, 4.5 TB/s) are bound by what each does one after the other, loads, meetings and
 // second reads, with four rows on a CU: neither twice the loads in flight nor a fifth fewer vector instructions made a difference.
 // Alternatives cost the pass three instructions per 16 bytes: a lane keeps its largest granule's place and the maximum of the
 // others.  Behind the pass groups of lanes meet, and the n-th largest of their maxima, tau, is at most the n-th largest logit:
@@ -688,8 +688,9 @@ __global__ __launch_bounds__(2 * kJoinMost) void logprobs_join_kernel(LogprobsPa
 }
 
 // Gradient: elementwise, one workgroup per kGradSteps * T granules of a row; the ids that fall into its share are looked for
-// once and kept in LDS, each with the sum of its gradients, in their order.  At an id the definition is a difference, of g and
-// p g of the same token, which is all that a confident target has: it is formed as g (1 - p) by itself.
+// once and kept in LDS, in their order, so that ids that repeat add up the same way every time.  At an id the definition is a
+// difference, of g and p g of the same token, which is all that a confident target has: of a token that has more than half it is
+// formed as g (1 - p) by itself.
 constexpr int kGradSteps = 4;
 
 struct GradRow {
@@ -706,11 +707,10 @@ struct GradRow {
         const float lp = log_prob(x);
         return by_others(__builtin_amdgcn_exp2f(lp * kLog2e), lp, factor);
     }
-    // 1 - p to its relative precision: log p over what the logarithm of the rounded p is (Kahan's correction)
-    __device__ __forceinline__ float at_id(float x, float g, float others) const {
-        const float lp = log_prob(x), p = __builtin_amdgcn_exp2f(lp * kLog2e);
-        float rest = 1.f - p;
-        if (p > 0.5f) rest = rest > 0.f ? rest * (lp * kLog2e) * __builtin_amdgcn_rcpf(__builtin_amdgcn_logf(p)) : -lp;
+    // A token of p > 1/2: 1 - p to its relative precision, by log p over what the logarithm of the rounded p is (Kahan's correction)
+    __device__ __forceinline__ float likely(float lp, float g, float others) const {
+        const float p = __builtin_amdgcn_exp2f(lp * kLog2e), seen = 1.f - p;
+        const float rest = seen > 0.f ? seen * (lp * kLog2e) * __builtin_amdgcn_rcpf(__builtin_amdgcn_logf(p)) : -lp;
         return fmaf(g, rest, by_others(p, lp, others));
     }
 };
@@ -728,7 +728,8 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
     const int v0 = first ? 0 : row.index(g0), v1 = last ? p.V : row.index(g1);
 
     __shared__ int hit_id[SPECEE_IDS_MAX], hits;
-    __shared__ float hit_g[SPECEE_IDS_MAX], hit_others[SPECEE_IDS_MAX], factor;
+    __shared__ int all_id[kWave];
+    __shared__ float hit_g[SPECEE_IDS_MAX], all_g[kWave], factor;
     if (tid < kWave) {
         int id = -1;
         float gt = 0.f;
@@ -737,23 +738,15 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
             if ((unsigned)id < (unsigned)p.V) gt = p.g_logprobs[(size_t)n * p.T + lane];
         }
         const float sum = wave_sum(gt);
-        float same = 0.f, others = 0.f;
-        bool repeated = false;
-        for (int t = 0; t < p.T; ++t) {
-            const bool eq = __builtin_amdgcn_readlane(id, t) == id;
-            const float g = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, gt), t));
-            same += eq ? g : 0.f;
-            others += eq ? 0.f : g;
-            repeated |= eq && t < lane;
-        }
-        const bool here = id >= v0 && id < v1 && !repeated;
+        const bool here = id >= v0 && id < v1;
         const unsigned long long who = __ballot(here);
         if (here) {
             const int at = __popcll(who & ((1ull << lane) - 1));
             hit_id[at] = id;
-            hit_g[at] = same;
-            hit_others[at] = others;
+            hit_g[at] = gt;
         }
+        all_id[lane] = id;
+        all_g[lane] = gt;
         if (lane == 0) {
             hits = __popcll(who);
             factor = sum;
@@ -781,6 +774,17 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
     f.factor = factor;
     const int H = hits;
     const bool empty = f.m == -INFINITY;  // no token has a probability: nothing to move
+    // d with the gradient g of its token x; of one that has more than half of all, from the sums of its own and the others'
+    auto with_id = [&](int id, float g, float x, float d) {
+        const float lp = f.log_prob(x);
+        if (!(lp > -kLn2)) return d + g;
+        float own = 0.f, others = 0.f;
+        for (int t = 0; t < p.T; ++t) {
+            own += all_id[t] == id ? all_g[t] : 0.f;
+            others += all_id[t] == id ? 0.f : all_g[t];
+        }
+        return f.likely(lp, own, others);
+    };
     const bool same = ((reinterpret_cast<uintptr_t>(out) ^ reinterpret_cast<uintptr_t>(row.p)) & 15) == 0;
 #pragma unroll
     for (int u = 0; u < kGradSteps; ++u) {
@@ -793,10 +797,13 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
             for (int h = 0; h < H; ++h) {
                 const int j0 = hit_id[h] - at;
                 if ((unsigned)j0 < (unsigned)G) {
-                    float xh = 0.f;
+                    float xh = 0.f, dh = 0.f;
 #pragma unroll
-                    for (int j = 0; j < G; ++j) xh = j == j0 ? (float)x[u].v[j] : xh;
-                    const float dh = f.at_id(xh, hit_g[h], hit_others[h]);
+                    for (int j = 0; j < G; ++j) {
+                        xh = j == j0 ? (float)x[u].v[j] : xh;
+                        dh = j == j0 ? d[j] : dh;
+                    }
+                    dh = with_id(hit_id[h], hit_g[h], xh, dh);
 #pragma unroll
                     for (int j = 0; j < G; ++j) d[j] = j == j0 ? dh : d[j];
                 }
@@ -817,7 +824,7 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
     if (extra >= 0) {
         float d = f(xe);
         for (int h = 0; h < H; ++h)
-            if (hit_id[h] == extra) d = f.at_id(xe, hit_g[h], hit_others[h]);
+            if (hit_id[h] == extra) d = with_id(extra, hit_g[h], xe, d);
         out[extra] = (E)(empty ? 0.f : d);
     }
 }
@@ -825,11 +832,12 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
 }  // namespace
 
 // How rows are dealt out: one workgroup per row, of 1024 threads where no CU has two rows and a row is long enough to give each
-// thread two steps (1 x 32000 fp32 with five alternatives 6.8 us, of 512 threads 7.8; 256 x 32000 10.0 and 10.8), else of 512
-// (511 x 32000 15.0 us, of 1024 threads 15.5; 1 x 8000 4.7 and 4.8), and of 256 where there are many short ones (one alternative,
-// 3317 x 777 fp32 18 -> 11 us, 4096 x 8000 28 -> 26, fp16 25 -> 19; but 600 x 8000 8.5 and 8.8, 2043 x 32003 43 and 46).  A few
-// rows of more than 224 KB in parts of at most 64 KB (fp16: 32 KB), which workgroups of 512 threads hold and a second launch joins
-// (1 x 128256 fp32 10.1 us, in one workgroup 14.3; 64 x 128256 14.8 and 16.3; but 100 x 128256 21 and 17, 1 x 50280 9.4 and 8.2).
+// thread two steps (256 x 32000 fp32 with five alternatives 9.6 us, of 512 threads 10.5; 1 x 32000 7.0 and 7.2), else of 512 (511
+// x 32000 14.7 us, of 1024 threads 15.7; 1 x 8000 5.1 of either), and of 256 where there are many short ones (one alternative,
+// 3317 x 777 fp32 11 us, of 512 threads 18.5; 4096 x 8000 27 and 30, fp16 21 and 29; but 600 x 8000 7.9 and 8.3, 2043 x 32003 46.9
+// and 45.3).  A few rows of more than 224 KB in parts of at most 64 KB (fp16: 32 KB), which workgroups of 512 threads hold and a
+// second launch joins (1 x 128256 fp32 8.6 us, in one workgroup 14.0; 64 x 128256 14.4 and 17.2, 80 would be 15.9 and 17.3, 100 17.8
+// and 17.5; 1 x 50280 8.2 and 8.1).
 namespace {
 struct Deal {
     int parts, threads, granules;  // granules per thread that are held; 0: in steps
@@ -843,8 +851,8 @@ Deal deal(int N, int V, bool half) {
     }
     return Deal{1, N <= 256 && whole > 2048 ? 1024 : N > 1024 && whole <= 2048 ? 256 : kT, 0};
 }
-// More than a few alternatives in kernels of their own (2043 x 8000 fp16, 20 alternatives: 22 us, in those for a few 26; five: 18
-// and 16.7)
+// More than a few alternatives, which is more than the fewest groups of lanes (16) could bear, in kernels of their own (2043 x 8000
+// fp16: 20 of them 19.4 us; five 14.7, in the kernels for many 15.9)
 constexpr int kFew = 8;
 template <typename E, bool MANY>
 hipError_t launch_rows(const LogprobsParams &p, const Deal &d, hipStream_t s) {
