@@ -258,7 +258,6 @@ struct LogprobsGradParams {
     const int32_t *ids;
     const float *max_logit, *log_sum, *entropy, *g_logprobs, *g_entropy;
     void *grad;
-    bool once;  // set by the launcher: gradients too large for any cache
 };
 constexpr int kLogprobsRowsInParts = 64;  // more rows are never cut into parts
 int logprobs_parts(int N, int V, bool half);

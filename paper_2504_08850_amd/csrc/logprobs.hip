@@ -715,7 +715,8 @@ struct GradRow {
     }
 };
 
-template <typename E, int T>
+// ONCE: gradients that no cache keeps until they are read
+template <typename E, int T, bool ONCE>
 __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) {
     constexpr int G = Granule<E>::n;
     const int n = blockIdx.y, tid = threadIdx.x, lane = tid & (kWave - 1);
@@ -812,7 +813,7 @@ __global__ __launch_bounds__(T) void logprobs_grad_kernel(LogprobsGradParams p) 
 #pragma unroll
             for (int j = 0; j < G; ++j) o.v[j] = (E)(empty ? 0.f : d[j]);
             if (same)
-                if (p.once)
+                if constexpr (ONCE)
                     __builtin_nontemporal_store(__builtin_bit_cast(uintx4, o), reinterpret_cast<uintx4 *>(out + at));
                 else
                     *reinterpret_cast<uintx4 *>(out + at) = __builtin_bit_cast(uintx4, o);
@@ -887,25 +888,29 @@ hipError_t launch_logprobs(const LogprobsParams &p, bool half, hipStream_t s) {
 }
 
 namespace {
-template <typename E, int T>
+template <typename E, int T, bool ONCE>
 hipError_t launch_grad(const LogprobsGradParams &p, int whole, hipStream_t s) {
     const int share = kGradSteps * T;
-    hipLaunchKernelGGL((logprobs_grad_kernel<E, T>), dim3(whole < 1 ? 1 : (whole + share - 1) / share, p.N), dim3(T), 0, s, p);
+    hipLaunchKernelGGL((logprobs_grad_kernel<E, T, ONCE>), dim3(whole < 1 ? 1 : (whole + share - 1) / share, p.N), dim3(T), 0, s, p);
     return hipGetLastError();
+}
+
+template <typename E>
+hipError_t launch_grad(const LogprobsGradParams &p, hipStream_t s) {
+    // no cache keeps more than this until it is read (4096 x 32000 fp16, 262 MB: 101 us without the hint, 91 with it; 128 MB of
+    // fp32 51.6 and 48.0, 96 MB of fp16 38.5 and 38.2; but 77 MB of fp32 29.0 and 30.6)
+    const bool once = (size_t)p.N * p.V * sizeof(E) > (96u << 20);
+    // many short rows by two wavefronts each (4096 x 1030 fp32 14.2 -> 9.4 us, 4096 x 2000 fp16 15.7 -> 10.4; but 60 x 777 2.9 and
+    // 3.2)
+    const int whole = p.V / Granule<E>::n;
+    if (p.N > 512 && whole <= kGradSteps * 128)
+        return once ? launch_grad<E, 128, true>(p, whole, s) : launch_grad<E, 128, false>(p, whole, s);
+    return once ? launch_grad<E, kT, true>(p, whole, s) : launch_grad<E, kT, false>(p, whole, s);
 }
 }  // namespace
 
-hipError_t launch_logprobs_grad(const LogprobsGradParams &params, bool half, hipStream_t s) {
-    // no cache keeps more than this from one pass to the next (4096 x 32000 fp16: 104 us without the hint, 94 with it;
-    // 60 x 32003 fp32: 6.2 and 7.3)
-    LogprobsGradParams p = params;
-    p.once = (size_t)p.N * p.V * (half ? 2 : 4) > (64u << 20);
-    // many short rows by two wavefronts each (4096 x 1030 fp32 13.9 -> 9.5 us, 4096 x 2000 fp16 15.6 -> 11.0; but 60 x 777 3.9 and
-    // 5.3)
-    const int whole = p.V / (half ? 8 : 4);
-    if (p.N > 512 && whole <= kGradSteps * 128)
-        return half ? launch_grad<half_t, 128>(p, whole, s) : launch_grad<float, 128>(p, whole, s);
-    return half ? launch_grad<half_t, kT>(p, whole, s) : launch_grad<float, kT>(p, whole, s);
+hipError_t launch_logprobs_grad(const LogprobsGradParams &p, bool half, hipStream_t s) {
+    return half ? launch_grad<half_t>(p, s) : launch_grad<float>(p, s);
 }
 
 }  // namespace specee

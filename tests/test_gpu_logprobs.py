@@ -457,6 +457,22 @@ def test_gradient_of_a_confident_target(sp, N, V, repeats, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("N,V,dtype", [(800, 32003, torch.float32), (1700, 32000, torch.float16), (30001, 1030, torch.float32),
+                                       (26000, 2050, torch.float16)])
+def test_gradients_too_large_for_a_cache(sp, N, V, dtype):
+    """100 MB and more: stores with the non-temporal hint, of rows by 512 and by 128 threads, in place too."""
+    ids = tokens(N, V, 2, 6)
+    g = torch.randn((N, 2), generator=torch.Generator().manual_seed(3))
+    y = logits(64, V, dtype, 4).cuda().repeat(-(-N // 64), 1)[:N].contiguous()
+    st = sp.logprobs(y)
+    got = sp.logprobs_grad(y, ids.cuda(), st["max_logit"], st["log_sum"], g_logprobs=g.cuda())
+    for rows in (slice(0, 40), slice(N // 2, N // 2 + 40), slice(N - 40, N)):
+        check_grad(got[rows], y[rows].cpu(), ids[rows], g[rows], None)
+    again = sp.logprobs_grad(y, ids.cuda(), st["max_logit"], st["log_sum"], g_logprobs=g.cuda(), out=y)
+    assert again.data_ptr() == y.data_ptr() and torch.equal(again, got)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
 def test_gradient_strides_alignments_and_places(sp, dtype):
     N, V = 3, 2053
