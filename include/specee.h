@@ -358,8 +358,8 @@ int specee_layer_loop_q4(const specee_dims *dims, int L, int B, const specee_hal
  *   x [N][d] or NULL: x rounded to fp16 (from s before its rounding); may be `branch` or `hidden` itself, not
  *   hidden_out.
  *   x8 [N][d], x8_scales [N][ceil(d/128)], both or neither NULL: x in 8 bits.  The 128 elements of a block
- *   (fewer in the last) share scale = max|x| / 448 (1 if they are all 0), and x8 = e4m3(x / scale), to nearest,
- *   ties to even.  A NaN stays one; an infinity makes its block NaN.
+ *   (fewer in the last) share scale = max|x| / 448 (1 if they are all 0, and a normal number at least), and
+ *   x8 = e4m3(x / scale), to nearest, ties to even.  A NaN stays one; an infinity makes its block NaN.
  * Only dims->d and dims->eps are read.  Needs no workspace.
  */
 int specee_block_norm(const specee_dims *dims, int N, const specee_half *hidden, const specee_half *branch,
@@ -375,7 +375,9 @@ int specee_block_norm(const specee_dims *dims, int N, const specee_half *hidden,
  *   the end may be shorter.  out, out_f16 [N][V]: one of them, the other NULL.
  * Products and sums are fp32.  For an fp32 result they are formed from the codes as halves, exactly; for an fp16 result
  * from the codes on the 8-bit matrix cores, which line products of 128 elements up with the largest of them: off by 1e-5 to
- * 5e-5 of the 2-norm of a block's products (up to 4e-4 for single sums), where fp16 rounds by up to 5e-4.
+ * 5e-5 of the 2-norm of a block's products (up to 4e-4 for single sums), where fp16 rounds by up to 5e-4.  Where that matters,
+ * ask for fp32 and round.  The order in which blocks are added is fixed for a call's sizes and type of result, the same for all
+ * its states; calls with another N may take another.
  * d: a multiple of 16, at most 65536; only dims->d and dims->V are read.
  * Workspace: SPECEE_OP_MATMUL_F8 with n = N, or the largest N that is to come.
  */
@@ -388,6 +390,7 @@ int specee_matmul_f8(const specee_dims *dims, int N, const specee_f8 *x, const f
  * probabilities of given tokens, the entropy, the best alternatives.  For each row, with m its largest logit
  * and S = sum exp(x - m):
  *     log p(v) = (x_v - m) - log S,      entropy = log S - sum exp(x - m)(x - m) / S.
+ * Where one token is all but certain, log S and the entropy are small, and exact to their own size.
  *   logits, logits_f16: one of them, the other NULL; row n starts `stride` elements (>= V) behind row n - 1.
  *   The pointer needs its type's alignment only.
  *   ids [N][T] (T up to SPECEE_IDS_MAX; 0: none, ids and logprobs NULL).

@@ -6,10 +6,10 @@
 // 5e-5 of their 2-norm, a tenth of what the result's own rounding is at that size.  fp32 results would show that: their codes become
 // halves first (exact) and are multiplied by the fp16 instruction (off by 1e-7), at twice the time per product.
 //
-// Few rows of x are a stream over w: 1 x 32000 x 4096 takes 23.5 us and 60 x 128256 x 8192 in fp32 197 us, 5.6 and 5.4 TB/s of w
+// Few rows of x are a stream over w: 1 x 32000 x 4096 takes 23.5 us and 60 x 128256 x 8192 in fp32 199 us, 5.6 and 5.3 TB/s of w
 // (a kernel that only reads gets 7.1).  Every tile reads x again (the latter in tiles of 128 rows: 217 us, 197 without the loads
 // of x), so higher tiles are taken where they leave no CU idle.  Many rows are bound by the overlap of a CU's loads with its
-// products: 8192 x 8192 x 8192 takes 513 us in fp16 (2.14 PFLOP/s), the products alone 415, the loads alone 400.
+// products: 8192 x 8192 x 8192 takes 520 us in fp16 (2.11 PFLOP/s; 513 to 531 between runs), the products alone 415, the loads alone 400.
 //
 // A workgroup's tile goes through its elements block by block.  Loads go to LDS without registers, one to two blocks ahead; a
 // meeting of the workgroup per block (two where x has one place less, see below) keeps them apart from the reads.
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(S::threads, 2) void matmul_f8_kernel(MatmulF8Params
     const Loader<S> load(p, v0, n0, wave, lane, f8_smem);
     // Rows of w that are read once: the workgroups begin at different elements and go round, since rows a power of
     // two apart have the same elements in few memory channels (60 states on 128256 x 8192, fp16 result: 226 -> 202 us).
-    // A result depends on its row of w alone, whatever N.
+    // The order is the same for all states of a call and every time; another N may take other tiles or parts, and so another order.
     const int turn = S::once ? (int)(blockIdx.x * 37u % (unsigned)(b1 - b0)) : 0;
     auto block = [&](int b) { return S::once && b + turn >= b1 ? b + turn - (b1 - b0) : b + turn; };
 
